@@ -1,0 +1,113 @@
+// The 8-bit paged cache: host plan of ragged rows, kernel arguments and the launchers.
+#pragma once
+
+#include <cstdint>
+#include <vector>
+
+#include "orthrus/kv8.h"
+
+namespace orthrus {
+
+constexpr int kPage8 = 16;         // positions of a page
+constexpr int kLeastExp8 = -100;   // least exponent of a page's scale
+constexpr int kSmallCols = 16;     // (row, query head) pairs of one small item: the columns of a 16x16 MFMA
+constexpr int kTileRows8 = 128;    // (row, query head) pairs of one tile of a longer segment
+
+// int32 fields of an attention item and of a merge entry (its rows, pieces and first partial slot);
+// partial slots hold 16 (row, head) pairs of head_dim + 2 floats each
+enum Item8 { A8_SEQ = 0, A8_ROW, A8_LEN, A8_POS, A8_HEAD, A8_KEY0, A8_KEY1, A8_SLOT, kItem8Ints };
+enum Merge8 { M8_ROW = 0, M8_LEN, M8_HEAD, M8_PIECES, M8_SLOT, M8_SLOTS, kMerge8Ints };
+// int32 fields of an append unit: the tokens of one segment that share a page
+enum Unit8 { U8_SEQ = 0, U8_BLOCK, U8_FIRST, U8_LEN, U8_ROW, kUnit8Ints };
+
+// pieces of long key ranges: at most this many more items than a plan without pieces has
+constexpr int kMaxSmallPieces = 1024, kMaxTilePieces = 512;
+
+// The uploaded plan, from ws + kPlanOffset on: int32 stamp, padding to 64 bytes, turns[64] (double:
+// turns per position of each pair, f_i / 2 pi), then units, small items, tile items, merges.
+constexpr size_t kPlanOffset = 256;
+constexpr int kTurnsInt = 16, kUnitsInt = kTurnsInt + 128;
+
+struct RowsPlan {
+    int T = 0, n_units = 0, n_small = 0, n_tiles = 0, n_merge = 0, n_slots = 0;
+    int most_merge_cols = 0;                    // (row, head) pairs of the largest merge entry
+    int need_seq = 0, need_blocks = 0;          // what a cache must have
+    std::vector<int32_t> meta;                  // uploaded verbatim
+    int off_small = 0, off_tiles = 0, off_merge = 0;
+};
+
+int validate_shape8(const orthrus_head_shape &s);
+int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, const orthrus_kv8 &kv,
+               const orthrus_segment *seg, int n, RowsPlan &out);
+// most meta ints and partial slots that a plan of these sizes can have
+void bound_rows8(const orthrus_head_shape &s, int64_t max_rows, int64_t max_segs, int64_t max_keys, size_t &meta_ints, size_t &slots);
+
+}  // namespace orthrus
+
+#ifdef __HIPCC__
+#include <hip/hip_runtime.h>
+
+#include "common.hpp"
+
+namespace orthrus {
+
+// what every kernel of a plan reads
+struct Plan8 {
+    const int32_t *meta;     // the uploaded plan
+    int stamp;               // the plan these arguments were made for
+    int *err;
+    uint8_t *k, *v;          // the layer's pools and scales
+    float *ks, *vs;
+    const int32_t *table;
+    int n_pages, max_blocks, nq, nkv, hd, group;
+};
+
+struct Append8 {
+    Plan8 p;
+    const void *qkv;
+    int64_t stride;
+    const float *q_gain, *k_gain;
+    void *q_out;
+    int64_t q_stride;
+    int n_units, rot, interleaved, in_dtype, out_dtype;
+    float magnitude, eps;
+};
+hipError_t launch_append8(const Append8 &a, hipStream_t s);
+
+struct Read8 {
+    Plan8 p;
+    int n_units;
+    bf16 *k_out, *v_out;
+};
+hipError_t launch_read8(const Read8 &a, hipStream_t s);
+
+struct Attend8 {
+    Plan8 p;
+    const void *q;
+    void *out;
+    int64_t q_stride, out_stride;
+    int dtype, n_small, n_tiles, n_merge, most_merge_cols, off_small, off_tiles, off_merge;
+    float scale;             // log2(e) times the softmax scale
+    float *partials;
+};
+hipError_t launch_attend8(const Attend8 &a, hipStream_t s);
+
+// a launch whose workspace holds another plan by now ends at once (replayed graphs)
+__device__ __forceinline__ bool stale8(const Plan8 &p) {
+    if (p.meta[0] == p.stamp) return false;
+    if (threadIdx.x == 0) flag_error(p.err, ORTHRUS_DEVERR_STALE);
+    return true;
+}
+
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+// two codes (the low or the high half of a word) as bf16 values times a power of two: exact
+template <bool HIGH> __device__ __forceinline__ uint32_t codes_bf16(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HIGH));
+}
+// four codes as four bf16 values
+__device__ __forceinline__ uint2 word_bf16(uint32_t w, float scale) {
+    return uint2{codes_bf16<false>(w, scale), codes_bf16<true>(w, scale)};
+}
+
+}  // namespace orthrus
+#endif

@@ -1,0 +1,346 @@
+// Head norms, rotation and append into the 8-bit cache, and the read-back of what it holds.
+//
+// One workgroup serves one append unit (the tokens of one segment that share a page) and one KV
+// head: that head's keys and values, and the query heads that read it.  A page's scale needs the
+// largest magnitude of all its tokens, and here they are all in one workgroup: keys and values go
+// from their rows to codes in registers, and only the values' tile, whose layout crosses tokens,
+// passes through LDS.
+//
+// A head row of HD dims lies over HD / 16 lanes; lane i holds dims 8 i .. 8 i + 7 and HD / 2 + 8 i ..
+// + 7, two 16-byte loads of bf16, so that the pairs (i, i + HD / 2) of a head that turns whole, and
+// the pairs (2 i, 2 i + 1), are in one lane; pairs of a head that turns in part meet through LDS.
+#include "kv8.hpp"
+
+namespace orthrus {
+namespace {
+
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+// over the LPR = 4 or 8 lanes of a head row (quad permutations, then the mirror of 8 lanes)
+template <int LPR> __device__ __forceinline__ float row_sum(float v) {
+    v += dpp<0xB1>(v);
+    v += dpp<0x4E>(v);
+    if (LPR == 8) v += dpp<0x141>(v);
+    return v;
+}
+template <int LPR> __device__ __forceinline__ float row_max(float v) {
+    v = fmaxf(v, dpp<0xB1>(v));
+    v = fmaxf(v, dpp<0x4E>(v));
+    if (LPR == 8) v = fmaxf(v, dpp<0x141>(v));
+    return v;
+}
+
+// the least power of two s with amax <= 448 s = 1.75 * 2^8 s, from amax's exponent and mantissa
+__device__ __forceinline__ float scale_of(float amax) {
+    const uint32_t b = __float_as_uint(amax);
+    int e = (int)(b >> 23) - 127 - 8;
+    if ((b & 0x7fffffu) > 0x600000u) ++e;
+    return __uint_as_float((uint32_t)(max(e, kLeastExp8) + 127) << 23);
+}
+
+template <typename T> __device__ __forceinline__ void load8(const T *p, float (&x)[8]);
+template <> __device__ __forceinline__ void load8<float>(const float *p, float (&x)[8]) {
+    const float4 a = *(const float4 *)p, b = *(const float4 *)(p + 4);
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+template <> __device__ __forceinline__ void load8<bf16>(const bf16 *p, float (&x)[8]) {
+    const u32x4 w = *(const u32x4 *)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = bf16_lo(w[i]);
+        x[2 * i + 1] = bf16_hi(w[i]);
+    }
+}
+__device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
+    *(float4 *)p = float4{x[0], x[1], x[2], x[3]};
+    *(float4 *)(p + 4) = float4{x[4], x[5], x[6], x[7]};
+}
+__device__ __forceinline__ void store8(bf16 *p, const float (&x)[8]) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+    *(u32x4 *)p = w;
+}
+
+// e4m3 codes of four values, rounded to nearest even; |x| <= 448 by the choice of the scale, what is
+// not finite becomes not a number
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+// the codes of a word times `ratio`, rounded again
+__device__ __forceinline__ uint32_t rescale4(uint32_t w, float ratio) {
+    const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    return encode4(lo[0] * ratio, lo[1] * ratio, hi[0] * ratio, hi[1] * ratio);
+}
+
+template <typename TI, typename TO, int HD>
+__global__ __launch_bounds__(256) void append8_kernel(Append8 a) {
+    constexpr int LPR = HD / 16;             // lanes of a head row
+    constexpr int GROUPS = 256 / LPR;        // head rows in flight
+    constexpr int DB = HD / 16;
+    static_assert(GROUPS >= 2 * kPage8, "keys and values of a page in one round");
+    __shared__ float2 turn[kPage8][HD / 2];            // (cos, sin) of each token and pair
+    __shared__ float swap[GROUPS][HD + 4];
+    __shared__ float amax[2][kPage8];
+    __shared__ __attribute__((aligned(16))) uint8_t tile[kPage8 * HD];
+    if (stale8(a.p)) return;
+    const int tid = threadIdx.x, g = blockIdx.x % a.p.nkv;
+    const int32_t *u = a.p.meta + kUnitsInt + kUnit8Ints * (int)(blockIdx.x / a.p.nkv);
+    const int seq = u[U8_SEQ], block = u[U8_BLOCK], first = u[U8_FIRST], n = u[U8_LEN], row0 = u[U8_ROW];
+    const int page = a.p.table[(size_t)seq * a.p.max_blocks + block];
+    const bool ok = page >= 0 && page < a.p.n_pages;
+    if (!ok && tid == 0) flag_error(a.p.err, ORTHRUS_DEVERR_PAGE);
+
+    const int half = a.rot / 2;
+    if (half > 0) {
+        const double *turns = (const double *)(a.p.meta + kTurnsInt);
+        for (int i = tid; i < n * half; i += 256) {
+            const int t = i / half, pr = i % half;
+            // turns modulo one in double: far positions keep their angle
+            const double x = (double)(block * kPage8 + first + t) * turns[pr];
+            const float f = (float)(2.0 * (x - rint(x)));
+            float sn, cs;
+            sincospif(f, &sn, &cs);
+            turn[t][pr] = float2{cs * a.magnitude, sn * a.magnitude};
+        }
+    }
+    __syncthreads();
+
+    const int grp = tid / LPR, i = tid % LPR;
+    // head row `h` of token t, normed and turned, in this lane's 16 dims (x[0]: 8 i .., x[1]: HD / 2 + 8 i ..)
+    auto head_row = [&](int t, int h, const float *gain, bool turns, float (&x)[2][8]) {
+        const TI *src = (const TI *)a.qkv + (size_t)(row0 + t) * a.stride + (size_t)h * HD + 8 * i;
+        load8(src, x[0]);
+        load8(src + HD / 2, x[1]);
+        if (gain) {
+            float ss = 0.f;
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) ss = fmaf(x[c][j], x[c][j], ss);
+            const float inv = 1.0f / sqrtf(row_sum<LPR>(ss) / (float)HD + a.eps);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float gv[8];
+                load8(gain + c * (HD / 2) + 8 * i, gv);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[c][j] = x[c][j] * inv * gv[j];
+            }
+        }
+        if (!turns || half == 0) return;
+        if (a.interleaved) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int d = c * (HD / 2) + 8 * i;
+                if (d < a.rot) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 cs = turn[t][d / 2 + j];
+                        const float p = x[c][2 * j], q = x[c][2 * j + 1];
+                        x[c][2 * j] = p * cs.x - q * cs.y;
+                        x[c][2 * j + 1] = q * cs.x + p * cs.y;
+                    }
+                }
+            }
+        } else if (a.rot == HD) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float2 cs = turn[t][8 * i + j];
+                const float p = x[0][j], q = x[1][j];
+                x[0][j] = p * cs.x - q * cs.y;
+                x[1][j] = q * cs.x + p * cs.y;
+            }
+        } else {
+            // pairs (d, d + rot / 2): the partner's eight dims from another lane of the row
+            float *mine = swap[grp];
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            store8(mine + 8 * i, x[0]);
+            store8(mine + HD / 2 + 8 * i, x[1]);
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int d = c * (HD / 2) + 8 * i;
+                if (d < a.rot) {
+                    const bool low = d < half;
+                    const int pr = low ? d : d - half;
+                    float other[8];
+                    load8((const float *)mine + (low ? d + half : d - half), other);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float2 cs = turn[t][pr + j];
+                        x[c][j] = low ? x[c][j] * cs.x - other[j] * cs.y : x[c][j] * cs.x + other[j] * cs.y;
+                    }
+                }
+            }
+        }
+    };
+
+    // keys and values: group t holds token t's key, group 16 + t its value
+    const int which = grp / kPage8, t = grp % kPage8;      // 0 key, 1 value
+    const bool live = which < 2 && t < n;
+    float x[2][8];
+    if (live) {
+        head_row(t, which == 0 ? a.p.nq + g : a.p.nq + a.p.nkv + g, which == 0 ? a.k_gain : nullptr, which == 0, x);
+        float m = 0.f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = fabsf(x[c][j]);
+                if (v < INFINITY) m = fmaxf(m, v);
+                else x[c][j] = NAN;
+            }
+        m = row_max<LPR>(m);
+        if (i == 0) amax[which][t] = m;
+    }
+    __syncthreads();
+    const size_t head = (size_t)(ok ? page : 0) * a.p.nkv + g;
+    uint8_t *kp = a.p.k + head * (kPage8 * HD), *vp = a.p.v + head * (kPage8 * HD);
+    float scale[2], was[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        float m = 0.f;
+        for (int s = 0; s < n; ++s) m = fmaxf(m, amax[w][s]);
+        scale[w] = scale_of(m);
+        was[w] = scale[w];
+        if (first > 0) {
+            was[w] = (w == 0 ? a.p.ks : a.p.vs)[head];
+            scale[w] = fmaxf(scale[w], was[w]);
+        }
+    }
+    if (live && ok) {
+        const float inv = 1.0f / scale[which];             // a power of two: exact
+        uint32_t c[2][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                c[h][j] = encode4(x[h][4 * j] * inv, x[h][4 * j + 1] * inv, x[h][4 * j + 2] * inv, x[h][4 * j + 3] * inv);
+        const int slot = first + t;
+        if (which == 0) {
+            *(uint2 *)(kp + slot * HD + 8 * i) = uint2{c[0][0], c[0][1]};
+            *(uint2 *)(kp + slot * HD + HD / 2 + 8 * i) = uint2{c[1][0], c[1][1]};
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int d = h * (HD / 2) + 8 * i + j;
+                    tile[(slot / 4) * (4 * HD) + (d % 16) * (4 * DB) + (d / 16) * 4 + slot % 4] = (uint8_t)(c[h][j / 4] >> (8 * (j % 4)));
+                }
+        }
+    }
+    __syncthreads();
+    if (ok) {
+        // the values' tile: wave q writes the four slots 4 q .. 4 q + 3; slots outside the unit keep their codes
+        // (rounded again where they came before it and the scale grew)
+        constexpr int W = HD / 64;                         // words a lane
+        const int q = tid / 64, lane = tid % 64;
+        const int lo = max(first - 4 * q, 0), hi = min(first + n - 4 * q, 4);      // new slots of the four
+        const bool again_v = scale[1] > was[1];
+        if (hi > 0 && (lo < 4 || again_v)) {
+            const uint32_t below = lo >= 4 ? 0xffffffffu : (1u << (8 * lo)) - 1;   // slots before the unit
+            const uint32_t fresh = lo >= 4 ? 0u : (hi >= 4 ? 0xffffffffu : (1u << (8 * hi)) - 1) & ~below;
+            uint32_t *dst = (uint32_t *)(vp + q * (4 * HD)) + W * lane;
+            const uint32_t *src = (const uint32_t *)(tile + q * (4 * HD)) + W * lane;
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                uint32_t w = src[j];
+                if (fresh != 0xffffffffu) {
+                    const uint32_t old = dst[j];
+                    const uint32_t kept = again_v ? rescale4(old, was[1] / scale[1]) : old;
+                    w = (w & fresh) | (kept & below) | (old & ~(fresh | below));
+                }
+                dst[j] = w;
+            }
+        }
+        if (scale[0] > was[0]) {
+            uint32_t *dst = (uint32_t *)kp;
+            for (int j = tid; j < first * HD / 4; j += 256) dst[j] = rescale4(dst[j], was[0] / scale[0]);
+        }
+        if (tid == 0) {
+            a.p.ks[head] = scale[0];
+            a.p.vs[head] = scale[1];
+        }
+    }
+
+    // the query heads of this KV head
+    const int rows = n * a.p.group;
+    for (int r = grp; r < rows; r += GROUPS) {
+        const int tq = r / a.p.group, h = g * a.p.group + r % a.p.group;
+        head_row(tq, h, a.q_gain, true, x);
+        TO *dst = (TO *)a.q_out + (size_t)(row0 + tq) * a.q_stride + (size_t)h * HD + 8 * i;
+        store8(dst, x[0]);
+        store8(dst + HD / 2, x[1]);
+    }
+}
+
+template <int HD> __global__ __launch_bounds__(256) void read8_kernel(Read8 a) {
+    constexpr int PT = HD / 16, DB = HD / 16;              // dims a thread
+    __shared__ __attribute__((aligned(16))) uint8_t tile[kPage8 * HD];
+    if (stale8(a.p)) return;
+    const int tid = threadIdx.x, g = blockIdx.x % a.p.nkv;
+    const int32_t *u = a.p.meta + kUnitsInt + kUnit8Ints * (int)(blockIdx.x / a.p.nkv);
+    const int seq = u[U8_SEQ], block = u[U8_BLOCK], first = u[U8_FIRST], n = u[U8_LEN], row0 = u[U8_ROW];
+    const int page = a.p.table[(size_t)seq * a.p.max_blocks + block];
+    const bool ok = page >= 0 && page < a.p.n_pages;
+    if (!ok && tid == 0) flag_error(a.p.err, ORTHRUS_DEVERR_PAGE);
+    const size_t head = (size_t)(ok ? page : 0) * a.p.nkv + g;
+    const uint8_t *kp = a.p.k + head * (kPage8 * HD), *vp = a.p.v + head * (kPage8 * HD);
+    for (int i = tid; i < kPage8 * HD / 8; i += 256) ((uint2 *)tile)[i] = ((const uint2 *)vp)[i];
+    __syncthreads();
+    const int t = tid / 16, slot = first + t, d0 = (tid % 16) * PT;
+    if (t >= n) return;
+    const float ks = ok ? a.p.ks[head] : 1.f, vs = ok ? a.p.vs[head] : 1.f;
+    uint32_t ow[2][PT / 2];
+#pragma unroll
+    for (int j = 0; j < PT / 4; ++j) {
+        const uint2 w = word_bf16(ok ? *(const uint32_t *)(kp + slot * HD + d0 + 4 * j) : 0u, ks);
+        ow[0][2 * j] = w.x;
+        ow[0][2 * j + 1] = w.y;
+        uint32_t c = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int d = d0 + 4 * j + e;
+            c |= (uint32_t)tile[(slot / 4) * (4 * HD) + (d % 16) * (4 * DB) + (d / 16) * 4 + slot % 4] << (8 * e);
+        }
+        const uint2 v = word_bf16(ok ? c : 0u, vs);
+        ow[1][2 * j] = v.x;
+        ow[1][2 * j + 1] = v.y;
+    }
+    const size_t at = (size_t)(row0 + t) * ((size_t)a.p.nkv * HD) + (size_t)g * HD + d0;
+#pragma unroll
+    for (int j = 0; j < PT / 4; ++j) {
+        *(uint2 *)(a.k_out + at + 4 * j) = uint2{ow[0][2 * j], ow[0][2 * j + 1]};
+        *(uint2 *)(a.v_out + at + 4 * j) = uint2{ow[1][2 * j], ow[1][2 * j + 1]};
+    }
+}
+
+template <typename TI, typename TO> void append_of(const Append8 &a, dim3 grid, hipStream_t s) {
+    if (a.p.hd == 64) hipLaunchKernelGGL((append8_kernel<TI, TO, 64>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((append8_kernel<TI, TO, 128>), grid, dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+hipError_t launch_append8(const Append8 &a, hipStream_t s) {
+    const dim3 grid(a.n_units * a.p.nkv);
+    if (a.in_dtype == ORTHRUS_BF16) append_of<bf16, bf16>(a, grid, s);
+    else if (a.out_dtype == ORTHRUS_BF16) append_of<float, bf16>(a, grid, s);
+    else append_of<float, float>(a, grid, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_read8(const Read8 &a, hipStream_t s) {
+    const dim3 grid(a.n_units * a.p.nkv);
+    if (a.p.hd == 64) hipLaunchKernelGGL(read8_kernel<64>, grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(read8_kernel<128>, grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace orthrus
