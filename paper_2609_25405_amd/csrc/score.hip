@@ -1,14 +1,17 @@
 // Scores of tokens under logits: log probability, entropy, rank and the largest entries of each row.
 //
-// A row is read once: a workgroup holds its slice in registers, so the maximum is known before the first
-// exponential and nothing is rescaled.  Rows of up to kSliceMost entries are one slice; longer ones,
-// and rows too few to fill the chip, are several, joined by a second launch of one wave a row.
+// A row is read once: a workgroup holds its slice of up to kSliceMost entries in registers, so the maximum is
+// known before the first exponential and nothing is rescaled.  Longer rows are several slices, joined by a
+// second launch of one wave a row.
 //
 // Order.  An entry's key is its value as an order-preserving integer (NaN above everything, -0 equal to +0) over the
-// complement of its index, so all keys differ and equal values rank by index.  The n largest of a
-// slice: every thread's best entry, sorted within each wave and merged over the waves (64 at a time,
-// bitonic), gives a bound that n entries reach; the n threads that reach it hold every entry that
-// can be among the n largest, and those few are sorted.
+// complement of its index, so all keys differ and equal values rank by index.
+// The n largest of a slice: the n-th largest of the maxima of 64 groups of threads is a bound that n entries reach;
+// the few that reach it (24 on average for n = 20) go to LDS as keys and one wave sorts them.
+// Rank: entries of a lower index count where they are not smaller than the token's, the others where they are larger.
+//
+// Slices with a NaN, an infinite maximum, more candidates than LDS holds (long ties) or a token whose own logit is not
+// finite take slice_by_keys: the same results from keys alone, read again, slower.
 #include <algorithm>
 
 #include "score.hpp"
@@ -78,13 +81,105 @@ __device__ void write_row(const Score &a, int r, int tok, float m, float z, floa
     }
 }
 
+constexpr int kCands = 1024;
+
+template <int NT> struct ScoreShared {
+    static constexpr int NW = NT / 64;
+    u64 cand[kCands];
+    u64 best[NT];                 // slice_by_keys
+    float group[64];
+    float red[3][NW];
+    int red_rank[NW], n_cand;
+};
+
+// a sum over the workgroup in the waves' order, for every thread
+template <int NT> __device__ __forceinline__ float block_total(const float *red) {
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) t += red[w];
+    return t;
+}
+
+// The slice [e0, e1) of row x by keys alone: every thread's largest key, the 64 largest of those (sorted in each wave, merged
+// over the waves), whose n-th is a bound; the at most 64 threads that reach it then pass their keys in
+// descending order, one at a time.
+template <int NT>
+__device__ void slice_by_keys(ScoreShared<NT> &sh, const float *x, int e0, int e1, int n, bool has, int tok, bool alone, float &m, float &z,
+                              float &s1, int &rank, u64 &key) {
+    constexpr int NW = NT / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const u64 tok_key = has ? key_of(order_of(x[tok]), tok) : 0;
+    u64 top = 0;
+    int before = 0;
+    for (int e = e0 + tid; e < e1; e += NT) {
+        const u64 k = key_of(order_of(x[e]), e);
+        top = k > top ? k : top;
+        before += has && k > tok_key ? 1 : 0;
+    }
+    __syncthreads();              // the fast path is done with what follows
+    u64 sorted = wave_sort(top, lane);
+    sh.best[tid] = sorted;
+    for (int half = NW / 2; half >= 1; half /= 2) {
+        __syncthreads();
+        if (wave < half) {
+            sorted = wave_merge(sorted, sh.best[(wave + half) * 64 + 63 - lane], lane);
+            sh.best[tid] = sorted;
+        }
+    }
+    __syncthreads();
+    m = value_of((uint32_t)(sh.best[0] >> 32));
+    const bool none = m == -INFINITY;      // nothing but -inf in the slice
+    z = s1 = 0.f;
+    for (int e = e0 + tid; e < e1; e += NT) {
+        const float v = x[e], d = v - m;
+        const float w = v == -INFINITY && !(none && alone) ? 0.f : __builtin_amdgcn_exp2f(d * 1.4426950408889634f);
+        z += w;
+        s1 += w > 0.f ? w * d : 0.f;
+    }
+    z = wave_sum(z);
+    s1 = wave_sum(s1);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) before += __shfl_xor(before, o, 64);
+    if (lane == 0) {
+        sh.red[0][wave] = z;
+        sh.red[1][wave] = s1;
+        sh.red_rank[wave] = before;
+    }
+    // n rounds: the largest key below the last one
+    u64 last = ~0ull;
+    key = 0;
+    for (int i = 0; i < n; ++i) {
+        u64 mine = top < last ? top : 0;
+        if (top >= last && top != 0) {     // this thread's largest is taken: its next
+            for (int e = e0 + tid; e < e1; e += NT) {
+                const u64 k = key_of(order_of(x[e]), e);
+                if (k < last && k > mine) mine = k;
+            }
+        }
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) {
+            const u64 p = shfl_xor64(mine, o);
+            mine = p > mine ? p : mine;
+        }
+        __syncthreads();
+        if (lane == 0) sh.best[wave] = mine;
+        __syncthreads();
+        last = 0;
+        for (int w = 0; w < NW; ++w) last = sh.best[w] > last ? sh.best[w] : last;
+        if (lane == i) key = last;
+        if (last == 0) break;              // fewer entries than n
+    }
+    __syncthreads();
+    z = block_total<NT>(sh.red[0]);
+    s1 = block_total<NT>(sh.red[1]);
+    rank = 0;
+    for (int w = 0; w < NW; ++w) rank += sh.red_rank[w];
+}
+
 template <int NT, int E>
-__global__ __launch_bounds__(NT) void score_kernel(Score a, int slices) {
-    constexpr int NW = NT / 64, EV = E / 4;
-    __shared__ u64 best[NT];
-    __shared__ u64 cand[64 * E];
-    __shared__ float red[3][NW];
-    __shared__ int red_rank[NW], n_cand;
+__global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, int slices) {
+    constexpr int NW = NT / 64, EV = E / 4, GL = NT / 64;      // GL lanes a group
+    __shared__ ScoreShared<NT> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int r = blockIdx.x / slices, slice = blockIdx.x % slices;
     const float *x = a.logits + (size_t)r * a.stride;
@@ -92,6 +187,8 @@ __global__ __launch_bounds__(NT) void score_kernel(Score a, int slices) {
     const int off = (int)(((uintptr_t)x >> 2) & 3);
     const int nvec = (a.vocab + off + 3) / 4;
     const int v0 = (int)((int64_t)slice * nvec / slices), v1 = (int)((int64_t)(slice + 1) * nvec / slices);
+    const int tok = a.tokens ? a.tokens[r] : -1;
+    const bool has = tok >= 0 && tok < a.vocab;
     float v[E];
 #pragma unroll
     for (int i = 0; i < EV; ++i) {
@@ -104,99 +201,96 @@ __global__ __launch_bounds__(NT) void score_kernel(Score a, int slices) {
             for (int j = 0; j < 4; ++j) v[4 * i + j] = q < v1 && e + j >= 0 && e + j < a.vocab ? x[e + j] : -INFINITY;
         }
     }
-    auto index = [&](int i) { return 4 * (v0 + i / 4 * NT + tid) - off + i % 4; };
-    auto real = [&](int i) { return v0 + i / 4 * NT + tid < v1 && index(i) >= 0 && index(i) < a.vocab; };
-    const int tok = a.tokens ? a.tokens[r] : -1;
-    const bool has = tok >= 0 && tok < a.vocab;
-    const uint32_t tok_order = has ? order_of(x[tok]) : 0;
-    u64 top = 0;
+    const float xt = has ? x[tok] : INFINITY;
+    if (tid == 0) sh.n_cand = 0;
+    float top = v[0];
+#pragma unroll
+    for (int i = 1; i < E; ++i) top = fmaxf(top, v[i]);
+    float gm = top;
+#pragma unroll
+    for (int o = 1; o < GL; o *= 2) gm = fmaxf(gm, __shfl_xor(gm, o, 64));
+    if (lane % GL == 0) sh.group[tid / GL] = gm;
+    __syncthreads();
+    gm = sh.group[lane];
+    const float m = wave_max(gm);
+    // entries before the token: the next smaller float turns "not smaller" into "larger"
+    const uint32_t tb = __float_as_uint(xt);
+    const float below = xt > 0.f ? __uint_as_float(tb - 1) : xt < 0.f ? __uint_as_float(tb + 1) : __uint_as_float(0x80000001u);
     int before = 0;
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-        const uint32_t o = order_of(v[i]);
-        const u64 k = real(i) ? key_of(o, index(i)) : 0;
-        top = k > top ? k : top;
-        before += has && k > key_of(tok_order, tok) ? 1 : 0;
-    }
-    if (tid == 0) n_cand = 0;
-    u64 sorted = 0;
-    if (a.n_top > 0) {
-        sorted = wave_sort(top, lane);
-        best[tid] = sorted;
-        for (int half = NW / 2; half >= 1; half /= 2) {
-            __syncthreads();
-            if (wave < half) {
-                sorted = wave_merge(sorted, best[(wave + half) * 64 + 63 - lane], lane);
-                best[tid] = sorted;
-            }
-        }
-        __syncthreads();
-    } else {
-        u64 m = top;
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) {
-            const u64 p = shfl_xor64(m, o);
-            m = p > m ? p : m;
-        }
-        if (lane == 0) best[wave] = m;
-        __syncthreads();
-        m = best[0];
-        for (int w = 1; w < NW; ++w) m = best[w] > m ? best[w] : m;
-        __syncthreads();
-        if (tid == 0) best[0] = m;
-        __syncthreads();
-    }
-    const float m = value_of((uint32_t)(best[0] >> 32));
-    const bool none = m == -INFINITY;      // nothing but -inf in the slice
-    if (a.n_top > 0) {
-        const u64 bound = best[a.n_top - 1];
-        if (top >= bound && top != 0) {
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const u64 k = real(i) ? key_of(order_of(v[i]), index(i)) : 0;
-                if (k >= bound && k != 0) cand[atomicAdd(&n_cand, 1)] = k;
-            }
-        }
-    }
     float z = 0.f, s1 = 0.f;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-        const float d = v[i] - m;
-        const float e = v[i] == -INFINITY && !(none && slices == 1) ? 0.f : __builtin_amdgcn_exp2f(d * 1.4426950408889634f);
-        z += e;
-        s1 += e > 0.f ? e * d : 0.f;       // (a weight of zero may have an infinite distance)
+    for (int i = 0; i < EV; ++i) {
+        const int e = 4 * (v0 + i * NT + tid) - off;
+        const bool lower = e + 3 < tok;
+        const float limit = lower ? below : xt;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float f = v[4 * i + j], d = f - m;
+            const float w = __builtin_amdgcn_exp2f(d * 1.4426950408889634f);
+            z += w;
+            s1 = fmaf(w, fmaxf(d, -200.f), s1);        // (a weight of zero may have an infinite distance)
+            before += f > limit ? 1 : 0;
+            if (!lower && e + j < tok && f == xt) ++before;       // the vector that holds the token
+        }
+    }
+    if (a.n_top > 0) {
+        // the n-th largest group maximum: its rank among the 64 (equal ones in lane order)
+        int larger = 0;
+#pragma unroll 8
+        for (int o = 0; o < 64; ++o) {
+            const float g = sh.group[o];
+            larger += g > gm || (g == gm && o < lane) ? 1 : 0;
+        }
+        const uint64_t nth = __ballot(larger == a.n_top - 1);
+        const float bound = __shfl(gm, nth ? __builtin_ctzll(nth) : 0, 64);
+        if (top >= bound) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const int e = 4 * (v0 + i / 4 * NT + tid) - off + i % 4;
+                if (v[i] >= bound && v[i] > -INFINITY) {
+                    const int c = atomicAdd(&sh.n_cand, 1);
+                    if (c < kCands) sh.cand[c] = key_of(order_of(v[i]), e);
+                }
+            }
+        }
     }
     z = wave_sum(z);
     s1 = wave_sum(s1);
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) before += __shfl_xor(before, o, 64);
     if (lane == 0) {
-        red[0][wave] = z;
-        red[1][wave] = s1;
-        red_rank[wave] = before;
+        sh.red[0][wave] = z;
+        sh.red[1][wave] = s1;
+        sh.red_rank[wave] = before;
     }
     __syncthreads();
-    if (wave != 0) return;
-    z = s1 = 0.f;
-    before = 0;
-    for (int w = 0; w < NW; ++w) {
-        z += red[0][w];
-        s1 += red[1][w];
-        before += red_rank[w];
-    }
+    z = block_total<NT>(sh.red[0]);
+    float mm = m;
     u64 key = 0;
-    if (a.n_top > 0) {
-        for (int c = 0; c < n_cand; c += 64) {
-            const u64 k = wave_sort(c + lane < n_cand ? cand[c + lane] : 0, lane);
-            key = c == 0 ? k : wave_merge(key, shfl64(k, 63 - lane), lane);
+    const int nc = sh.n_cand;
+    // (block-uniform: every thread has read the same sums)
+    if (!(z < INFINITY) || (has && !(fabsf(xt) < INFINITY)) || nc > kCands || nc < a.n_top) {
+        slice_by_keys<NT>(sh, x, max(4 * v0 - off, 0), min(4 * v1 - off, a.vocab), a.n_top, has, tok, slices == 1, mm, z, s1, before, key);
+        if (wave != 0) return;
+    } else {
+        if (wave != 0) return;
+        s1 = block_total<NT>(sh.red[1]);
+        before = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) before += sh.red_rank[w];
+        if (a.n_top > 0) {
+            for (int c = 0; c < nc; c += 64) {
+                const u64 k = wave_sort(c + lane < nc ? sh.cand[c + lane] : 0, lane);
+                key = c == 0 ? k : wave_merge(key, shfl64(k, 63 - lane), lane);
+            }
         }
     }
     if (slices == 1) {
-        write_row(a, r, tok, m, z, s1, before, key, lane);
+        write_row(a, r, tok, mm, z, s1, before, key, lane);
         return;
     }
     char *pp = a.ws + (size_t)blockIdx.x * part_bytes(a.n_top);
-    if (lane == 0) *(Part *)pp = Part{m, z, s1, before};
+    if (lane == 0) *(Part *)pp = Part{mm, z, s1, before};
     if (lane < a.n_top) ((u64 *)(pp + sizeof(Part)))[lane] = key;
 }
 
@@ -232,12 +326,7 @@ __global__ __launch_bounds__(64) void score_merge_kernel(Score a, int slices) {
 
 }  // namespace
 
-int score_slices(int rows, int vocab) {
-    const int least = (vocab + 3 + kSliceMost - 1) / kSliceMost;
-    // few rows: slices of at least 4096 entries until the chip's 256 CUs have one each
-    const int more = std::min((256 + rows - 1) / rows, vocab / 4096);
-    return std::max({1, least, more});
-}
+int score_slices(int rows, int vocab) { return (vocab + 3 + kSliceMost - 1) / kSliceMost; }
 
 size_t score_bytes(int rows, int vocab, int n_top) {
     const int s = score_slices(rows, vocab);
