@@ -16,6 +16,9 @@
 
 #include "score.hpp"
 
+// a reference r = L x is the rounded product wherever it is used: no contraction but the written fused operations
+#pragma clang fp contract(off)
+
 namespace orthrus {
 namespace {
 
@@ -34,50 +37,116 @@ __device__ __forceinline__ float value_of(uint32_t o) {
 __device__ __forceinline__ u64 key_of(uint32_t order, int idx) { return (u64)order << 32 | (uint32_t)~idx; }
 __device__ __forceinline__ int index_of(u64 key) { return (int)~(uint32_t)key; }
 
-__device__ __forceinline__ u64 shfl_xor64(u64 v, int m) {
-    const uint32_t lo = __shfl_xor((uint32_t)v, m, 64), hi = __shfl_xor((uint32_t)(v >> 32), m, 64);
-    return (u64)hi << 32 | lo;
+// lane ^ M by DPP and half-swaps (no LDS permutes)
+template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false);
 }
-__device__ __forceinline__ u64 shfl64(u64 v, int lane) {
-    const uint32_t lo = __shfl((uint32_t)v, lane, 64), hi = __shfl((uint32_t)(v >> 32), lane, 64);
-    return (u64)hi << 32 | lo;
+template <int M> __device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
+    if constexpr (M == 1) return dpp<0xB1>(v);                    // quad permutations
+    else if constexpr (M == 2) return dpp<0x4E>(v);
+    else if constexpr (M == 4) return dpp<0x1B>(dpp<0x141>(v));   // mirror of 8 (xor 7), then of 4 (xor 3)
+    else if constexpr (M == 8) return dpp<0x128>(v);              // rotation by 8 within 16
+    else if constexpr (M == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return (threadIdx.x & 16) ? r[0] : r[1];
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return (threadIdx.x & 32) ? r[0] : r[1];
+    }
+}
+template <int M> __device__ __forceinline__ u64 lane_xor64(u64 v) {
+    return (u64)lane_xor<M>((uint32_t)(v >> 32)) << 32 | lane_xor<M>((uint32_t)v);
+}
+template <int M> __device__ __forceinline__ float lane_xorf(float v) { return __uint_as_float(lane_xor<M>(__float_as_uint(v))); }
+__device__ __forceinline__ u64 wave_max64(u64 v) {
+    u64 o;
+    o = lane_xor64<1>(v), v = o > v ? o : v;
+    o = lane_xor64<2>(v), v = o > v ? o : v;
+    o = lane_xor64<4>(v), v = o > v ? o : v;
+    o = lane_xor64<8>(v), v = o > v ? o : v;
+    o = lane_xor64<16>(v), v = o > v ? o : v;
+    o = lane_xor64<32>(v), v = o > v ? o : v;
+    return v;
+}
+__device__ __forceinline__ float wave_addf(float v) {
+    v += lane_xorf<1>(v);
+    v += lane_xorf<2>(v);
+    v += lane_xorf<4>(v);
+    v += lane_xorf<8>(v);
+    v += lane_xorf<16>(v);
+    return v + lane_xorf<32>(v);
+}
+__device__ __forceinline__ int wave_addi(int v) {
+    v += (int)lane_xor<1>((uint32_t)v);
+    v += (int)lane_xor<2>((uint32_t)v);
+    v += (int)lane_xor<4>((uint32_t)v);
+    v += (int)lane_xor<8>((uint32_t)v);
+    v += (int)lane_xor<16>((uint32_t)v);
+    return v + (int)lane_xor<32>((uint32_t)v);
+}
+__device__ __forceinline__ float wave_maxf(float v) {
+    v = fmaxf(v, lane_xorf<1>(v));
+    v = fmaxf(v, lane_xorf<2>(v));
+    v = fmaxf(v, lane_xorf<4>(v));
+    v = fmaxf(v, lane_xorf<8>(v));
+    v = fmaxf(v, lane_xorf<16>(v));
+    return fmaxf(v, lane_xorf<32>(v));
+}
+__device__ __forceinline__ u64 reversed64(u64 v) {
+    const int lane = 63 - (threadIdx.x & 63);
+    return (u64)__shfl((uint32_t)(v >> 32), lane, 64) << 32 | __shfl((uint32_t)v, lane, 64);
 }
 // 64 keys, one a lane, in descending order: the whole bitonic sort, or its last stage (of a bitonic sequence)
-__device__ __forceinline__ u64 wave_stage(u64 v, int k, int lane) {
-    for (int j = k / 2; j > 0; j /= 2) {
-        const u64 o = shfl_xor64(v, j);
-        const bool high = ((lane & j) == 0) == ((lane & k) == 0);
-        v = (v > o) == high ? v : o;
-    }
-    return v;
+template <int J> __device__ __forceinline__ u64 wave_step(u64 v, int k, int lane) {
+    const u64 o = lane_xor64<J>(v);
+    return (v > o) == (((lane & J) == 0) == ((lane & k) == 0)) ? v : o;
+}
+template <int K> __device__ __forceinline__ u64 wave_stage(u64 v, int lane) {
+    if constexpr (K >= 64) v = wave_step<32>(v, K, lane);
+    if constexpr (K >= 32) v = wave_step<16>(v, K, lane);
+    if constexpr (K >= 16) v = wave_step<8>(v, K, lane);
+    if constexpr (K >= 8) v = wave_step<4>(v, K, lane);
+    if constexpr (K >= 4) v = wave_step<2>(v, K, lane);
+    return wave_step<1>(v, K, lane);
 }
 __device__ __forceinline__ u64 wave_sort(u64 v, int lane) {
-    for (int k = 2; k <= 64; k *= 2) v = wave_stage(v, k, lane);
-    return v;
+    v = wave_stage<2>(v, lane);
+    v = wave_stage<4>(v, lane);
+    v = wave_stage<8>(v, lane);
+    v = wave_stage<16>(v, lane);
+    v = wave_stage<32>(v, lane);
+    return wave_stage<64>(v, lane);
 }
 // the 64 largest of two descending runs of 64 (`other` read in reverse)
 __device__ __forceinline__ u64 wave_merge(u64 mine, u64 other_reversed, int lane) {
-    return wave_stage(mine > other_reversed ? mine : other_reversed, 64, lane);
+    return wave_stage<64>(mine > other_reversed ? mine : other_reversed, lane);
 }
+
+// Sums are held in base 2^L, L = log2(e) as an fp32 number: with a reference r near L max x, z = sum 2^(L x - r) and
+// s = sum (L x - r) 2^(L x - r), so that log Z = (r + log2 z) / L and the entropy is (log2 z - s / z) / L whatever r's own
+// rounding; L x - r is one fused operation.  What L differs from log2(e) by is a factor 1 + 1.3e-8 on the logits.
+constexpr float kL = 1.4426950408889634f;
+constexpr float kLeastT = -300.f;      // exponents below it weigh nothing, and minus infinity must not meet that zero
 
 // what a slice leaves to the merge launch, in the workspace: one Part, then n_top keys
 struct Part {
-    float m, z, s1;
-    int rank;
+    double r;      // L times a finite maximum, or the maximum (not finite)
+    float z, s;
+    int rank, pad;
 };
 __host__ __device__ __forceinline__ size_t part_bytes(int n_top) { return sizeof(Part) + 8 * (size_t)n_top; }
 
-__device__ void write_row(const Score &a, int r, int tok, float m, float z, float s1, int rank, u64 key, int lane) {
-    const float logz = logf(z);
+__device__ void write_row(const Score &a, int r, int tok, const Part &p, u64 key, int lane) {
+    const double logz = (p.r + (double)log2f(p.z)) / (double)kL;
     if (lane == 0) {
         const bool has = a.tokens && tok >= 0 && tok < a.vocab;
-        if (a.logprob) a.logprob[r] = has ? a.logits[(size_t)r * a.stride + tok] - m - logz : NAN;
-        if (a.rank) a.rank[r] = has ? rank : -1;
-        if (a.entropy) a.entropy[r] = logz - s1 / z;
+        if (a.logprob) a.logprob[r] = has ? (float)((double)a.logits[(size_t)r * a.stride + tok] - logz) : NAN;
+        if (a.rank) a.rank[r] = has ? p.rank : -1;
+        if (a.entropy) a.entropy[r] = (log2f(p.z) - p.s / p.z) / kL;
     }
     if (lane < a.n_top) {
         if (a.top_ids) a.top_ids[(size_t)r * a.n_top + lane] = index_of(key);
-        if (a.top_logprobs) a.top_logprobs[(size_t)r * a.n_top + lane] = value_of((uint32_t)(key >> 32)) - m - logz;
+        if (a.top_logprobs) a.top_logprobs[(size_t)r * a.n_top + lane] = (float)((double)value_of((uint32_t)(key >> 32)) - logz);
     }
 }
 
@@ -88,7 +157,8 @@ template <int NT> struct ScoreShared {
     u64 cand[kCands];
     u64 best[NT];                 // slice_by_keys
     float group[64];
-    float red[3][NW];
+    int larger[64];
+    float red[2][NW];
     int red_rank[NW], n_cand;
 };
 
@@ -104,8 +174,8 @@ template <int NT> __device__ __forceinline__ float block_total(const float *red)
 // over the waves), whose n-th is a bound; the at most 64 threads that reach it then pass their keys in
 // descending order, one at a time.
 template <int NT>
-__device__ void slice_by_keys(ScoreShared<NT> &sh, const float *x, int e0, int e1, int n, bool has, int tok, bool alone, float &m, float &z,
-                              float &s1, int &rank, u64 &key) {
+__device__ void slice_by_keys(ScoreShared<NT> &sh, const float *x, int e0, int e1, int n, bool has, int tok, bool alone, Part &p,
+                              u64 &key) {
     constexpr int NW = NT / 64;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const u64 tok_key = has ? key_of(order_of(x[tok]), tok) : 0;
@@ -127,22 +197,21 @@ __device__ void slice_by_keys(ScoreShared<NT> &sh, const float *x, int e0, int e
         }
     }
     __syncthreads();
-    m = value_of((uint32_t)(sh.best[0] >> 32));
+    const float m = value_of((uint32_t)(sh.best[0] >> 32));
     const bool none = m == -INFINITY;      // nothing but -inf in the slice
-    z = s1 = 0.f;
+    float z = 0.f, s = 0.f;
     for (int e = e0 + tid; e < e1; e += NT) {
-        const float v = x[e], d = v - m;
-        const float w = v == -INFINITY && !(none && alone) ? 0.f : __builtin_amdgcn_exp2f(d * 1.4426950408889634f);
+        const float v = x[e], t = (v - m) * kL;
+        const float w = v == -INFINITY && !(none && alone) ? 0.f : __builtin_amdgcn_exp2f(t);
         z += w;
-        s1 += w > 0.f ? w * d : 0.f;
+        s = fmaf(w, fmaxf(t, kLeastT), s);
     }
-    z = wave_sum(z);
-    s1 = wave_sum(s1);
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) before += __shfl_xor(before, o, 64);
+    z = wave_addf(z);
+    s = wave_addf(s);
+    before = wave_addi(before);
     if (lane == 0) {
         sh.red[0][wave] = z;
-        sh.red[1][wave] = s1;
+        sh.red[1][wave] = s;
         sh.red_rank[wave] = before;
     }
     // n rounds: the largest key below the last one
@@ -156,11 +225,7 @@ __device__ void slice_by_keys(ScoreShared<NT> &sh, const float *x, int e0, int e
                 if (k < last && k > mine) mine = k;
             }
         }
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) {
-            const u64 p = shfl_xor64(mine, o);
-            mine = p > mine ? p : mine;
-        }
+        mine = wave_max64(mine);
         __syncthreads();
         if (lane == 0) sh.best[wave] = mine;
         __syncthreads();
@@ -170,24 +235,26 @@ __device__ void slice_by_keys(ScoreShared<NT> &sh, const float *x, int e0, int e
         if (last == 0) break;              // fewer entries than n
     }
     __syncthreads();
-    z = block_total<NT>(sh.red[0]);
-    s1 = block_total<NT>(sh.red[1]);
-    rank = 0;
-    for (int w = 0; w < NW; ++w) rank += sh.red_rank[w];
+    p.r = (double)m * (double)kL;
+    p.z = block_total<NT>(sh.red[0]);
+    p.s = block_total<NT>(sh.red[1]);
+    p.rank = 0;
+    for (int w = 0; w < NW; ++w) p.rank += sh.red_rank[w];
 }
 
 template <int NT, int E>
 __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, int slices) {
     constexpr int NW = NT / 64, EV = E / 4, GL = NT / 64;      // GL lanes a group
+    constexpr int CH = E < 8 ? E : 8;
     __shared__ ScoreShared<NT> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int r = blockIdx.x / slices, slice = blockIdx.x % slices;
-    const float *x = a.logits + (size_t)r * a.stride;
+    const int row = blockIdx.x / slices, slice = blockIdx.x % slices;
+    const float *x = a.logits + (size_t)row * a.stride;
     // 16-byte loads from the aligned address at or before the row; elements outside the row are not read
     const int off = (int)(((uintptr_t)x >> 2) & 3);
     const int nvec = (a.vocab + off + 3) / 4;
     const int v0 = (int)((int64_t)slice * nvec / slices), v1 = (int)((int64_t)(slice + 1) * nvec / slices);
-    const int tok = a.tokens ? a.tokens[r] : -1;
+    const int tok = a.tokens ? a.tokens[row] : -1;
     const bool has = tok >= 0 && tok < a.vocab;
     float v[E];
 #pragma unroll
@@ -203,94 +270,121 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
     }
     const float xt = has ? x[tok] : INFINITY;
     if (tid == 0) sh.n_cand = 0;
-    float top = v[0];
-#pragma unroll
-    for (int i = 1; i < E; ++i) top = fmaxf(top, v[i]);
-    float gm = top;
-#pragma unroll
-    for (int o = 1; o < GL; o *= 2) gm = fmaxf(gm, __shfl_xor(gm, o, 64));
-    if (lane % GL == 0) sh.group[tid / GL] = gm;
-    __syncthreads();
-    gm = sh.group[lane];
-    const float m = wave_max(gm);
+    if (tid < 64) sh.larger[tid] = 0;
+    // eight entries at a time, as they arrive, under a reference of the thread's own
+    float top = -1e37f, z = 0.f, s = 0.f, r0 = -1e37f * kL;
     // entries before the token: the next smaller float turns "not smaller" into "larger"
     const uint32_t tb = __float_as_uint(xt);
     const float below = xt > 0.f ? __uint_as_float(tb - 1) : xt < 0.f ? __uint_as_float(tb + 1) : __uint_as_float(0x80000001u);
     int before = 0;
-    float z = 0.f, s1 = 0.f;
 #pragma unroll
-    for (int i = 0; i < EV; ++i) {
-        const int e = 4 * (v0 + i * NT + tid) - off;
-        const bool lower = e + 3 < tok;
-        const float limit = lower ? below : xt;
+    for (int c = 0; c < E; c += CH) {
+        float mc = v[c];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float f = v[4 * i + j], d = f - m;
-            const float w = __builtin_amdgcn_exp2f(d * 1.4426950408889634f);
+        for (int j = 1; j < CH; ++j) mc = fmaxf(mc, v[c + j]);
+        if (mc > top) {
+            top = mc;
+            const float r1 = mc * kL, f = __builtin_amdgcn_exp2f(r0 - r1);
+            s = f * fmaf(z, r0 - r1, s);
+            z *= f;
+            r0 = r1;
+        }
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const float t = fmaf(v[c + j], kL, -r0), w = __builtin_amdgcn_exp2f(t);
             z += w;
-            s1 = fmaf(w, fmaxf(d, -200.f), s1);        // (a weight of zero may have an infinite distance)
-            before += f > limit ? 1 : 0;
-            if (!lower && e + j < tok && f == xt) ++before;       // the vector that holds the token
+            s = fmaf(w, fmaxf(t, kLeastT), s);
+        }
+        if (has) {
+#pragma unroll
+            for (int i = c / 4; i < (c + CH) / 4; ++i) {
+                const int e = 4 * (v0 + i * NT + tid) - off;
+                const float limit = e + 3 < tok ? below : xt;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) before += v[4 * i + j] > limit ? 1 : 0;
+                if (e < tok && e + 3 >= tok) {                   // the vector that holds the token
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) before += e + j < tok && v[4 * i + j] == xt ? 1 : 0;
+                }
+            }
         }
     }
-    if (a.n_top > 0) {
-        // the n-th largest group maximum: its rank among the 64 (equal ones in lane order)
+    float gm = top;
+    if constexpr (GL >= 2) gm = fmaxf(gm, lane_xorf<1>(gm));
+    if constexpr (GL >= 4) gm = fmaxf(gm, lane_xorf<2>(gm));
+    if constexpr (GL >= 8) gm = fmaxf(gm, lane_xorf<4>(gm));
+    if constexpr (GL >= 16) gm = fmaxf(gm, lane_xorf<8>(gm));
+    if (lane % GL == 0) sh.group[tid / GL] = gm;
+    __syncthreads();
+    gm = sh.group[lane];
+    const float m = wave_maxf(gm), r = m * kL;
+    {
+        const float f = __builtin_amdgcn_exp2f(r0 - r);
+        s = f * fmaf(z, fmaxf(r0 - r, kLeastT), s);
+        z *= f;
+    }
+    z = wave_addf(z);
+    s = wave_addf(s);
+    before = wave_addi(before);
+    if (lane == 0) {
+        sh.red[0][wave] = z;
+        sh.red[1][wave] = s;
+        sh.red_rank[wave] = before;
+    }
+    if (a.n_top > 1) {
+        // how many group maxima are larger (equal ones in group order): each wave compares with its share of the 64
         int larger = 0;
-#pragma unroll 8
-        for (int o = 0; o < 64; ++o) {
+#pragma unroll
+        for (int o = wave * (64 / NW); o < (wave + 1) * (64 / NW); ++o) {
             const float g = sh.group[o];
             larger += g > gm || (g == gm && o < lane) ? 1 : 0;
         }
-        const uint64_t nth = __ballot(larger == a.n_top - 1);
-        const float bound = __shfl(gm, nth ? __builtin_ctzll(nth) : 0, 64);
+        if (larger) atomicAdd(&sh.larger[lane], larger);
+    }
+    __syncthreads();
+    if (a.n_top > 0) {
+        float bound = m;
+        if (a.n_top > 1) {
+            const uint64_t nth = __ballot(sh.larger[lane] == a.n_top - 1);
+            bound = __shfl(gm, nth ? __builtin_ctzll(nth) : 0, 64);
+        }
         if (top >= bound) {
 #pragma unroll
             for (int i = 0; i < E; ++i) {
                 const int e = 4 * (v0 + i / 4 * NT + tid) - off + i % 4;
-                if (v[i] >= bound && v[i] > -INFINITY) {
+                if (v[i] >= bound) {
                     const int c = atomicAdd(&sh.n_cand, 1);
                     if (c < kCands) sh.cand[c] = key_of(order_of(v[i]), e);
                 }
             }
         }
+        __syncthreads();
     }
-    z = wave_sum(z);
-    s1 = wave_sum(s1);
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) before += __shfl_xor(before, o, 64);
-    if (lane == 0) {
-        sh.red[0][wave] = z;
-        sh.red[1][wave] = s1;
-        sh.red_rank[wave] = before;
-    }
-    __syncthreads();
-    z = block_total<NT>(sh.red[0]);
-    float mm = m;
+    Part p{(double)r, block_total<NT>(sh.red[0]), 0.f, 0, 0};
     u64 key = 0;
     const int nc = sh.n_cand;
     // (block-uniform: every thread has read the same sums)
-    if (!(z < INFINITY) || (has && !(fabsf(xt) < INFINITY)) || nc > kCands || nc < a.n_top) {
-        slice_by_keys<NT>(sh, x, max(4 * v0 - off, 0), min(4 * v1 - off, a.vocab), a.n_top, has, tok, slices == 1, mm, z, s1, before, key);
+    if (!(p.z > 0.f && p.z < INFINITY) || (has && !(fabsf(xt) < INFINITY)) || nc > kCands || nc < a.n_top) {
+        slice_by_keys<NT>(sh, x, max(4 * v0 - off, 0), min(4 * v1 - off, a.vocab), a.n_top, has, tok, slices == 1, p, key);
         if (wave != 0) return;
     } else {
         if (wave != 0) return;
-        s1 = block_total<NT>(sh.red[1]);
-        before = 0;
+        p.s = block_total<NT>(sh.red[1]);
 #pragma unroll
-        for (int w = 0; w < NW; ++w) before += sh.red_rank[w];
+        for (int w = 0; w < NW; ++w) p.rank += sh.red_rank[w];
         if (a.n_top > 0) {
             for (int c = 0; c < nc; c += 64) {
                 const u64 k = wave_sort(c + lane < nc ? sh.cand[c + lane] : 0, lane);
-                key = c == 0 ? k : wave_merge(key, shfl64(k, 63 - lane), lane);
+                key = c == 0 ? k : wave_merge(key, reversed64(k), lane);
             }
         }
     }
     if (slices == 1) {
-        write_row(a, r, tok, mm, z, s1, before, key, lane);
+        write_row(a, row, tok, p, key, lane);
         return;
     }
     char *pp = a.ws + (size_t)blockIdx.x * part_bytes(a.n_top);
-    if (lane == 0) *(Part *)pp = Part{mm, z, s1, before};
+    if (lane == 0) *(Part *)pp = p;
     if (lane < a.n_top) ((u64 *)(pp + sizeof(Part)))[lane] = key;
 }
 
@@ -299,46 +393,53 @@ __global__ __launch_bounds__(64) void score_merge_kernel(Score a, int slices) {
     const int r = blockIdx.x, lane = threadIdx.x;
     const char *pp = a.ws + (size_t)r * slices * part_bytes(a.n_top);
     auto part = [&](int s) { return (const Part *)(pp + s * part_bytes(a.n_top)); };
-    float m = -INFINITY;
-    for (int s = 0; s < slices; ++s) m = part(s)->m > m || part(s)->m != part(s)->m ? part(s)->m : m;
-    float z = 0.f, s1 = 0.f;
-    int before = 0;
+    Part p{-INFINITY, 0.f, 0.f, 0, 0};
     for (int s = 0; s < slices; ++s) {
-        const Part p = *part(s);
-        const float d = p.m - m, f = __builtin_amdgcn_exp2f(d * 1.4426950408889634f);
-        if (p.m != -INFINITY) {
-            z += p.z * f;
-            s1 += f > 0.f ? f * (p.s1 + p.z * d) : 0.f;
-        }
-        before += p.rank;
+        const double r = part(s)->r;
+        p.r = r > p.r || r != r ? r : p.r;
     }
-    if (m == -INFINITY) z = NAN;
+    for (int s = 0; s < slices; ++s) {
+        const Part q = *part(s);
+        p.rank += q.rank;
+        if (q.r == -INFINITY) continue;                // nothing but -inf in the slice
+        const float d = (float)(q.r - p.r), f = __builtin_amdgcn_exp2f(d);
+        p.z += q.z * f;
+        p.s += f * (q.s + q.z * fmaxf(d, kLeastT));
+    }
+    if (p.r == -INFINITY) p.z = NAN;
     u64 key = 0;
     const int total = slices * a.n_top;
     for (int c = 0; c < total; c += 64) {
         const int i = c + lane;
         const u64 k = i < total ? ((const u64 *)(part(i / a.n_top) + 1))[i % a.n_top] : 0;
         const u64 sorted = wave_sort(k, lane);
-        key = c == 0 ? sorted : wave_merge(key, shfl64(sorted, 63 - lane), lane);
+        key = c == 0 ? sorted : wave_merge(key, reversed64(sorted), lane);
     }
-    write_row(a, r, a.tokens ? a.tokens[r] : -1, m, z, s1, before, key, lane);
+    write_row(a, r, a.tokens ? a.tokens[r] : -1, p, key, lane);
 }
 
 }  // namespace
 
-int score_slices(int rows, int vocab) { return (vocab + 3 + kSliceMost - 1) / kSliceMost; }
+namespace {
+// slices of a row that starts `off` entries past a 16-byte boundary
+int slices_of(int vocab, int off) { return (vocab + off + kSliceMost - 1) / kSliceMost; }
+}  // namespace
+
+int score_slices(int vocab) { return slices_of(vocab, 3); }
 
 size_t score_bytes(int rows, int vocab, int n_top) {
-    const int s = score_slices(rows, vocab);
+    const int s = score_slices(vocab);
     return s == 1 ? 0 : (size_t)rows * s * part_bytes(n_top);
 }
 
 hipError_t launch_score(const Score &a, hipStream_t s) {
-    const int slices = score_slices(a.rows, a.vocab);
-    const int entries = ((a.vocab + 6) / 4 + slices - 1) / slices * 4;       // of the longest slice, with the row's misalignment
+    const bool aligned = ((uintptr_t)a.logits & 15) == 0 && a.stride % 4 == 0;
+    const int off = aligned ? 0 : 3, slices = slices_of(a.vocab, off);
+    const int entries = ((a.vocab + off + 3) / 4 + slices - 1) / slices * 4;       // of the longest slice
     const dim3 grid(a.rows * slices);
     if (entries <= 1024) hipLaunchKernelGGL((score_kernel<256, 4>), grid, dim3(256), 0, s, a, slices);
     else if (entries <= 8192) hipLaunchKernelGGL((score_kernel<1024, 8>), grid, dim3(1024), 0, s, a, slices);
+    else if (entries <= 16384) hipLaunchKernelGGL((score_kernel<1024, 16>), grid, dim3(1024), 0, s, a, slices);
     else hipLaunchKernelGGL((score_kernel<1024, 32>), grid, dim3(1024), 0, s, a, slices);
     if (slices > 1) hipLaunchKernelGGL(score_merge_kernel, dim3(a.rows), dim3(64), 0, s, a, slices);
     return hipGetLastError();
@@ -361,7 +462,7 @@ int orthrus_logprobs(const float *logits, int64_t row_stride, int32_t rows, int3
     if (rows < 0 || vocab < 1 || n_top < 0 || n_top > std::min(vocab, ORTHRUS_MAX_TOP) || row_stride < vocab) return ORTHRUS_EINVAL;
     if (rows == 0) return ORTHRUS_OK;
     if (!logits || ((logprob || rank) && !tokens) || (n_top == 0 && (top_ids || top_logprobs))) return ORTHRUS_EINVAL;
-    if (vocab > (1 << 30) || (int64_t)rows * score_slices(rows, vocab) > INT32_MAX) return ORTHRUS_ECAPACITY;
+    if (vocab > (1 << 30) || (int64_t)rows * score_slices(vocab) > INT32_MAX) return ORTHRUS_ECAPACITY;
     const size_t need = score_bytes(rows, vocab, n_top);
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 15))) return ORTHRUS_EINVAL;
     if (ws_bytes < need) return ORTHRUS_ECAPACITY;

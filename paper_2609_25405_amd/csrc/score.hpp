@@ -16,8 +16,8 @@ struct Score {
     float *top_logprobs;
     char *ws;
 };
-// slices of a row that each get a workgroup; 1: no workspace and no merge launch
-int score_slices(int rows, int vocab);
+// most slices of a row, each a workgroup; 1: no workspace and no merge launch
+int score_slices(int vocab);
 size_t score_bytes(int rows, int vocab, int n_top);
 hipError_t launch_score(const Score &a, hipStream_t s);
 

@@ -31,19 +31,25 @@ def _need(ok: bool, what: str) -> None:
         raise A.OrthrusError(A.ORTHRUS_EINVAL, what)
 
 
-def _here(*tensors) -> None:
-    """Device tensors of a call belong to the current device, whose stream it is enqueued on."""
+# A call costs the host about as much as a small launch costs the device, so the checks below are few
+# and cheap: plain integers for pointers, one device query, one stream query, cached structs.
+def _here(*tensors) -> int:
+    """The current device, to which the device tensors of a call belong (its stream is the default one)."""
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -2     # (-1: a host tensor)
     for t in tensors:
-        if t is not None:
-            _need(t.is_cuda and t.device.index == torch.cuda.current_device(), "tensor on another device than the current one")
+        if t is not None and t.get_device() != dev:
+            raise A.OrthrusError(A.ORTHRUS_EINVAL, "tensor on another device than the current one")
+    return dev
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
-def _stream(stream):
-    return c_void_p(current_stream() if stream is None else stream)
+def _stream(stream, dev=None):
+    if stream is not None:
+        return stream
+    return current_stream() if dev is None else torch._C._cuda_getCurrentRawStream(dev)
 
 
 class HeadShape:
@@ -93,19 +99,33 @@ class DeviceKV8:
         _need(k_scale.dtype == v_scale.dtype == torch.float32 and k_scale.shape == v_scale.shape == (L, P, nkv), "scales")
         _need(block_table.dtype == torch.int32 and block_table.dim() == 2, "block table")
         _need(all(t.is_contiguous() for t in (k, v, k_scale, v_scale, block_table)), "contiguous cache tensors")
-        self.shape, self.k, self.v, self.k_scale, self.v_scale, self.block_table = shape, k, v, k_scale, v_scale, block_table
+        self.shape, self._tensors = shape, (k, v, k_scale, v_scale, block_table)
         self.n_layers, self.n_pages = L, P
         self.n_seq, self.max_blocks = block_table.shape
+        self._device = k.get_device()
+        _need(all(t.get_device() == self._device for t in self._tensors), "cache tensors on one device")
+        self._struct = O.orthrus_kv8(*[t.data_ptr() for t in self._tensors], L, P, self.n_seq, self.max_blocks)
+        self._ref = byref(self._struct)
+
+    # the tensors stay the ones the cache was made of
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    k_scale = property(lambda self: self._tensors[2])
+    v_scale = property(lambda self: self._tensors[3])
+    block_table = property(lambda self: self._tensors[4])
 
     def set_block_table(self, bt: np.ndarray) -> None:
         self.block_table.copy_(torch.from_numpy(np.ascontiguousarray(bt, np.int32)))
 
     def struct(self) -> O.orthrus_kv8:
-        return O.orthrus_kv8(_ptr(self.k), _ptr(self.v), _ptr(self.k_scale), _ptr(self.v_scale), _ptr(self.block_table),
-                             self.n_layers, self.n_pages, self.n_seq, self.max_blocks)
+        return O.orthrus_kv8.from_buffer_copy(self._struct)
 
     def _fits(self, shape: HeadShape) -> None:
-        _need((shape.n_kv_heads, shape.head_dim) == (self.shape.n_kv_heads, self.shape.head_dim), "cache of other heads")
+        if shape is not self.shape:
+            _need((shape.n_kv_heads, shape.head_dim) == (self.shape.n_kv_heads, self.shape.head_dim), "cache of other heads")
+
+    def _on(self, dev: int) -> None:
+        _need(self._device == dev, "cache on another device than the current one")
 
 
 def _segments(segments):
@@ -130,30 +150,31 @@ class RaggedRows:
         if torch.device(device).type == "cuda":
             self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
             _here(self.buf)
-            _check(A.orthrus_workspace_init(_ptr(self.buf), _stream(None)), "orthrus_workspace_init")
+            _check(A.orthrus_workspace_init(c_void_p(self.buf.data_ptr()), c_void_p(_stream(None))), "orthrus_workspace_init")
 
     def plan(self, kv: DeviceKV8, segments, stream: Optional[int] = None) -> None:
         """Plan the rows: (sequence, offset, length) of each segment, in the order of their rows."""
         kv._fits(self.shape)
-        _here(self.buf, kv.k, kv.v, kv.k_scale, kv.v_scale, kv.block_table)
+        dev = _here(self.buf)
+        kv._on(dev)
         seg = _segments(segments)
-        _check(O.load().orthrus_rows_plan(self.handle, byref(kv.struct()), c_void_p(seg.ctypes.data), len(seg), _ptr(self.buf),
-                                          self.nbytes, _stream(stream)), "orthrus_rows_plan")
+        _check(O.load().orthrus_rows_plan(self.handle, kv._ref, seg.ctypes.data, len(seg), _ptr(self.buf), self.nbytes,
+                                          _stream(stream, dev)), "orthrus_rows_plan")
         self.n_rows = int(seg[:, 2].sum())
 
     def items(self, kv: DeviceKV8, segments):
         """(counts, items[n, 8]) of a plan, on the host alone (orthrus_rows_items)."""
         seg = _segments(segments)
         counts = (c_int32 * 4)()
-        args = (self.handle, byref(kv.struct()), c_void_p(seg.ctypes.data), len(seg))
+        args = (self.handle, kv._ref, seg.ctypes.data, len(seg))
         _check(O.load().orthrus_rows_items(*args, counts, None, 0), "orthrus_rows_items")
         items = np.zeros((counts[0] + counts[1], 8), np.int32)
-        _check(O.load().orthrus_rows_items(*args, counts, c_void_p(items.ctypes.data), len(items)), "orthrus_rows_items")
+        _check(O.load().orthrus_rows_items(*args, counts, items.ctypes.data, len(items)), "orthrus_rows_items")
         return list(counts), items
 
     def device_error(self) -> int:
         bits = c_int32(0)
-        rc = A.orthrus_device_error(_ptr(self.buf), _stream(None), byref(bits))
+        rc = A.orthrus_device_error(c_void_p(self.buf.data_ptr()), c_void_p(_stream(None)), byref(bits))
         if rc not in (A.ORTHRUS_OK, A.ORTHRUS_EDEVICE):
             raise A.OrthrusError(rc, "orthrus_device_error")
         return bits.value
@@ -171,15 +192,20 @@ class RaggedRows:
 
     def _rows_of(self, t: torch.Tensor, width: int, dtype, what: str) -> int:
         """Row stride of a call's tensor: [rows or more][width], elements of a row side by side."""
-        _need(t.dtype == dtype and t.dim() == 2 and t.shape[1] == width and t.shape[0] >= self.n_rows, what + " shape")
-        _need(t.shape[1] == 1 or t.stride(1) == 1, what + " strides")
-        return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width)
+        n, w = t.shape if t.dim() == 2 else (0, 0)
+        if t.dtype != dtype or w != width or n < self.n_rows:
+            raise A.OrthrusError(A.ORTHRUS_EINVAL, what + " shape")
+        stride, inner = t.stride()
+        if inner != 1:
+            raise A.OrthrusError(A.ORTHRUS_EINVAL, what + " strides")
+        return stride if n > 1 else max(stride, width)
 
 
 def _gain(t, hd):
-    if t is not None:
-        _need(t.dtype == torch.float32 and t.shape == (hd,) and t.is_contiguous(), "gain shape")
-    return _ptr(t)
+    if t is None:
+        return None
+    _need(t.dtype == torch.float32 and t.shape == (hd,) and t.is_contiguous(), "gain shape")
+    return t.data_ptr()
 
 
 def kv8_append(rows: RaggedRows, kv: DeviceKV8, layer: int, qkv: torch.Tensor, q_out: torch.Tensor,
@@ -188,25 +214,30 @@ def kv8_append(rows: RaggedRows, kv: DeviceKV8, layer: int, qkv: torch.Tensor, q
     shape's dtype, or fp32); the rotated queries go to q_out [rows][n_q hd]."""
     s = rows.shape
     kv._fits(s)
-    _here(qkv, q_out, q_gain, k_gain, kv.k)
-    _need(qkv.dtype in (torch.float32, s.torch_dtype), "qkv dtype")
+    dev = _here(qkv, q_out, q_gain, k_gain)
+    kv._on(dev)
+    f32 = qkv.dtype == torch.float32
     width = (s.n_q_heads + 2 * s.n_kv_heads) * s.head_dim
-    stride, q_stride = rows._rows_of(qkv, width, qkv.dtype, "qkv"), rows._rows_of(q_out, s.n_q_heads * s.head_dim, s.torch_dtype, "q_out")
-    code = A.ORTHRUS_F32 if qkv.dtype == torch.float32 else A.ORTHRUS_BF16
-    _check(O.load().orthrus_kv8_append(rows.handle, byref(kv.struct()), layer, _ptr(qkv), code, stride, _gain(q_gain, s.head_dim),
-                                       _gain(k_gain, s.head_dim), _ptr(q_out), q_stride, _stream(stream)), "orthrus_kv8_append")
+    stride = rows._rows_of(qkv, width, torch.float32 if f32 else s.torch_dtype, "qkv")
+    q_stride = rows._rows_of(q_out, s.n_q_heads * s.head_dim, s.torch_dtype, "q_out")
+    rc = O.load().orthrus_kv8_append(rows.handle, kv._ref, layer, qkv.data_ptr(), A.ORTHRUS_F32 if f32 else A.ORTHRUS_BF16, stride,
+                                     _gain(q_gain, s.head_dim), _gain(k_gain, s.head_dim), q_out.data_ptr(), q_stride,
+                                     _stream(stream, dev))
+    _check(rc, "orthrus_kv8_append")
 
 
 def kv8_read(rows: RaggedRows, kv: DeviceKV8, layer: int, k_out: torch.Tensor, v_out: torch.Tensor,
              stream: Optional[int] = None) -> None:
     """What the cache holds at the planned rows' positions, as bf16 [rows][n_kv hd] (exact)."""
     kv._fits(rows.shape)
-    _here(k_out, v_out, kv.k)
+    dev = _here(k_out, v_out)
+    kv._on(dev)
     width = rows.shape.n_kv_heads * rows.shape.head_dim
     for t in (k_out, v_out):
-        rows._rows_of(t, width, torch.bfloat16, "read-back")
-        _need(t.is_contiguous(), "contiguous read-back")
-    _check(O.load().orthrus_kv8_read(rows.handle, byref(kv.struct()), layer, _ptr(k_out), _ptr(v_out), _stream(stream)), "orthrus_kv8_read")
+        if rows._rows_of(t, width, torch.bfloat16, "read-back") != width:
+            raise A.OrthrusError(A.ORTHRUS_EINVAL, "contiguous read-back")
+    _check(O.load().orthrus_kv8_read(rows.handle, kv._ref, layer, k_out.data_ptr(), v_out.data_ptr(), _stream(stream, dev)),
+           "orthrus_kv8_read")
 
 
 def kv8_attend(rows: RaggedRows, kv: DeviceKV8, layer: int, q: torch.Tensor, out: torch.Tensor, scale: Optional[float] = None,
@@ -215,12 +246,13 @@ def kv8_attend(rows: RaggedRows, kv: DeviceKV8, layer: int, q: torch.Tensor, out
     None: 1 / sqrt(hd)."""
     s = rows.shape
     kv._fits(s)
-    _here(q, out, kv.k)
+    dev = _here(q, out)
+    kv._on(dev)
     _need(scale is None or scale > 0, "scale")
     width = s.n_q_heads * s.head_dim
     stride, out_stride = rows._rows_of(q, width, s.torch_dtype, "q"), rows._rows_of(out, width, s.torch_dtype, "out")
-    _check(O.load().orthrus_kv8_attend(rows.handle, byref(kv.struct()), layer, _ptr(q), stride, scale or 0.0, _ptr(out), out_stride,
-                                       _stream(stream)), "orthrus_kv8_attend")
+    _check(O.load().orthrus_kv8_attend(rows.handle, kv._ref, layer, q.data_ptr(), stride, scale or 0.0, out.data_ptr(), out_stride,
+                                       _stream(stream, dev)), "orthrus_kv8_attend")
 
 
 def logprobs_workspace(rows: int, vocab: int, n_top: int = 0, device="cuda") -> Optional[torch.Tensor]:
@@ -237,14 +269,14 @@ def logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, logpro
     _need(logits.dtype == torch.float32 and logits.dim() == 2 and (logits.shape[1] == 1 or logits.stride(1) == 1), "logits")
     R, V = logits.shape
     tops = [t for t in (top_ids, top_logprobs) if t is not None]
-    _need(all(t.dim() == 2 and t.shape[0] == R and t.shape[1] == tops[0].shape[1] and t.shape[1] > 0 for t in tops), "top outputs")
-    n = tops[0].shape[1] if tops else 0
-    for t, dt in ((tokens, torch.int32), (rank, torch.int32), (top_ids, torch.int32), (logprob, torch.float32),
-                  (entropy, torch.float32), (top_logprobs, torch.float32)):
-        if t is not None:
-            _need(t.dtype == dt and t.is_contiguous() and t.shape[0] == R and (t.dim() == 1 or t is top_ids or t is top_logprobs), "score tensors")
-    _here(logits, tokens, logprob, entropy, rank, top_ids, top_logprobs, workspace)
+    n = tops[0].shape[-1] if tops else 0
+    _need(not tops or n > 0, "top outputs")
+    for t, dt, shape in ((tokens, torch.int32, (R,)), (rank, torch.int32, (R,)), (logprob, torch.float32, (R,)),
+                         (entropy, torch.float32, (R,)), (top_ids, torch.int32, (R, n)), (top_logprobs, torch.float32, (R, n))):
+        if t is not None and not (t.dtype == dt and t.shape == shape and t.is_contiguous()):
+            raise A.OrthrusError(A.ORTHRUS_EINVAL, "score tensors")
+    dev = _here(logits, tokens, logprob, entropy, rank, top_ids, top_logprobs, workspace)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     stride = logits.stride(0) if R > 1 else max(V, logits.stride(0))
     _check(O.load().orthrus_logprobs(_ptr(logits), stride, R, V, _ptr(tokens), n, _ptr(logprob), _ptr(entropy), _ptr(rank),
-                                     _ptr(top_ids), _ptr(top_logprobs), _ptr(workspace), ws_bytes, _stream(stream)), "orthrus_logprobs")
+                                     _ptr(top_ids), _ptr(top_logprobs), _ptr(workspace), ws_bytes, _stream(stream, dev)), "orthrus_logprobs")

@@ -139,7 +139,7 @@ def test_score_refusals():
     assert call(rows=0, logits=None) == A.ORTHRUS_OK
     b = lib.orthrus_logprobs_bytes
     assert b(0, 8, 1) == b(1, 0, 1) == b(1, 8, 9) == b(1, 8, -1) == b(1, 1000, 65) == 0
-    assert b(300, 32000, 20) == 0 and b(1, 32000, 20) > 0 and b(300, 128000, 64) > 0
+    assert b(300, 32000, 20) == b(1, 32000, 20) == 0 and b(1, 40000, 20) > 0 and b(300, 128000, 64) > 0
     with code_of(A.ORTHRUS_EINVAL):
         ops.logprobs(x[:16].view(2, 8).double())
     with code_of(A.ORTHRUS_EINVAL):
