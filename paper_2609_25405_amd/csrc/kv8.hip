@@ -125,7 +125,7 @@ size_t orthrus_rows_workspace_bytes(const orthrus_rows *r, int32_t max_rows, int
     if (!r || max_rows < 0 || max_segments < 0 || max_keys < 0) return 0;
     size_t ints = 0, slots = 0;
     bound_rows8(r->shape, max_rows, max_segments, max_keys, ints, slots);
-    return kPlanOffset + up256(ints * 4) + slots * kSmallCols * (size_t)(r->shape.head_dim + 2) * 4;
+    return kPlanOffset + up256(ints * 4) + slots * kSmallCols * (size_t)(r->shape.head_dim + kPartialPad) * 4;
 }
 
 int orthrus_rows_items(const orthrus_rows *r, const orthrus_kv8 *kv, const orthrus_segment *segments, int32_t n,
@@ -159,7 +159,7 @@ int orthrus_rows_plan(orthrus_rows *r, const orthrus_kv8 *kv, const orthrus_segm
         const int rc = plan_rows8(r->shape, r->turns, *kv, segments, n, p);
         if (rc) return rc;
         const size_t meta = up256(p.meta.size() * 4);
-        if (ws_bytes < kPlanOffset + meta + (size_t)p.n_slots * kSmallCols * (r->shape.head_dim + 2) * 4) return ORTHRUS_ECAPACITY;
+        if (ws_bytes < kPlanOffset + meta + (size_t)p.n_slots * kSmallCols * (r->shape.head_dim + kPartialPad) * 4) return ORTHRUS_ECAPACITY;
         hipStream_t s = (hipStream_t)stream;
         hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
         HIP_TRY(hipStreamIsCapturing(s, &cap));
@@ -258,7 +258,9 @@ int orthrus_kv8_attend(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t lay
     a.n_small = r->plan.n_small;
     a.n_tiles = r->plan.n_tiles;
     a.n_merge = r->plan.n_merge;
-    a.most_merge_cols = r->plan.most_merge_cols;
+    a.merge_slots = r->plan.merge_slots;
+    a.small_cols = r->plan.small_cols;
+    a.wide = r->plan.wide;
     a.off_small = r->plan.off_small;
     a.off_tiles = r->plan.off_tiles;
     a.off_merge = r->plan.off_merge;

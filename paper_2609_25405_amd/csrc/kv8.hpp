@@ -13,15 +13,17 @@ constexpr int kLeastExp8 = -100;   // least exponent of a page's scale
 constexpr int kSmallCols = 16;     // (row, query head) pairs of one small item: the columns of a 16x16 MFMA
 constexpr int kTileRows8 = 128;    // (row, query head) pairs of one tile of a longer segment
 
-// int32 fields of an attention item and of a merge entry (its rows, pieces and first partial slot);
-// partial slots hold 16 (row, head) pairs of head_dim + 2 floats each
+// int32 fields of an attention item and of a merge entry: the rows and head of a range that comes in pieces, how many,
+// the first partial slot and the slots of a piece
 enum Item8 { A8_SEQ = 0, A8_ROW, A8_LEN, A8_POS, A8_HEAD, A8_KEY0, A8_KEY1, A8_SLOT, kItem8Ints };
 enum Merge8 { M8_ROW = 0, M8_LEN, M8_HEAD, M8_PIECES, M8_SLOT, M8_SLOTS, kMerge8Ints };
+// a partial slot holds 16 (row, head) pairs: maximum, sum, two words of padding, head_dim sums
+constexpr int kPartialPad = 4;
 // int32 fields of an append unit: the tokens of one segment that share a page
 enum Unit8 { U8_SEQ = 0, U8_BLOCK, U8_FIRST, U8_LEN, U8_ROW, kUnit8Ints };
 
-// pieces of long key ranges: at most this many more items than a plan without pieces has
-constexpr int kMaxSmallPieces = 1024, kMaxTilePieces = 512;
+// pieces of long key ranges: at most so many a plan, and of one range
+constexpr int kMaxSmallPieces = 2048, kMaxTilePieces = 1024, kMaxPieces = 128;
 
 // The uploaded plan, from ws + kPlanOffset on: int32 stamp, padding to 64 bytes, turns[64] (double:
 // turns per position of each pair, f_i / 2 pi), then units, small items, tile items, merges.
@@ -30,7 +32,9 @@ constexpr int kTurnsInt = 16, kUnitsInt = kTurnsInt + 128;
 
 struct RowsPlan {
     int T = 0, n_units = 0, n_small = 0, n_tiles = 0, n_merge = 0, n_slots = 0;
-    int most_merge_cols = 0;                    // (row, head) pairs of the largest merge entry
+    int merge_slots = 0;                        // slots of a piece, the most of any merge entry
+    int small_cols = 0;                         // (row, head) pairs of the largest small item
+    int wide = 0;                               // few small items: more waves each
     int need_seq = 0, need_blocks = 0;          // what a cache must have
     std::vector<int32_t> meta;                  // uploaded verbatim
     int off_small = 0, off_tiles = 0, off_merge = 0;
@@ -86,17 +90,24 @@ struct Attend8 {
     const void *q;
     void *out;
     int64_t q_stride, out_stride;
-    int dtype, n_small, n_tiles, n_merge, most_merge_cols, off_small, off_tiles, off_merge;
+    int dtype, n_small, n_tiles, n_merge, merge_slots, small_cols, wide, off_small, off_tiles, off_merge;
     float scale;             // log2(e) times the softmax scale
     float *partials;
 };
 hipError_t launch_attend8(const Attend8 &a, hipStream_t s);
 
-// a launch whose workspace holds another plan by now ends at once (replayed graphs)
-__device__ __forceinline__ bool stale8(const Plan8 &p) {
-    if (p.meta[0] == p.stamp) return false;
+// The entry at `at` of the plan, or false where the workspace holds another plan by now (replayed graphs): then the workgroup
+// ends.  The entry is read before the comparison, so that the two latencies overlap; in any plan it is in bounds.
+template <int N> struct Entry8 { int32_t v[N]; };
+template <int N> __device__ __forceinline__ bool entry8(const Plan8 &p, int at, Entry8<N> &e) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) e.v[i] = p.meta[at + i];
+    const int stamp = p.meta[0];
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+s"(e.v[i]));       // (the loads stay ahead of the branch)
+    if (stamp == p.stamp) return true;
     if (threadIdx.x == 0) flag_error(p.err, ORTHRUS_DEVERR_STALE);
-    return true;
+    return false;
 }
 
 typedef float f32x2_t __attribute__((ext_vector_type(2)));

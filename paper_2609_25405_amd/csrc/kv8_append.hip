@@ -85,9 +85,10 @@ __global__ __launch_bounds__(256) void append8_kernel(Append8 a) {
     __shared__ float swap[GROUPS][HD + 4];
     __shared__ float amax[2][kPage8];
     __shared__ __attribute__((aligned(16))) uint8_t tile[kPage8 * HD];
-    if (stale8(a.p)) return;
     const int tid = threadIdx.x, g = blockIdx.x % a.p.nkv;
-    const int32_t *u = a.p.meta + kUnitsInt + kUnit8Ints * (int)(blockIdx.x / a.p.nkv);
+    Entry8<kUnit8Ints> entry;
+    if (!entry8(a.p, kUnitsInt + kUnit8Ints * (int)(blockIdx.x / a.p.nkv), entry)) return;
+    const int32_t *u = entry.v;
     const int seq = u[U8_SEQ], block = u[U8_BLOCK], first = u[U8_FIRST], n = u[U8_LEN], row0 = u[U8_ROW];
     const int page = a.p.table[(size_t)seq * a.p.max_blocks + block];
     const bool ok = page >= 0 && page < a.p.n_pages;
@@ -283,9 +284,10 @@ __global__ __launch_bounds__(256) void append8_kernel(Append8 a) {
 template <int HD> __global__ __launch_bounds__(256) void read8_kernel(Read8 a) {
     constexpr int PT = HD / 16, DB = HD / 16;              // dims a thread
     __shared__ __attribute__((aligned(16))) uint8_t tile[kPage8 * HD];
-    if (stale8(a.p)) return;
     const int tid = threadIdx.x, g = blockIdx.x % a.p.nkv;
-    const int32_t *u = a.p.meta + kUnitsInt + kUnit8Ints * (int)(blockIdx.x / a.p.nkv);
+    Entry8<kUnit8Ints> entry;
+    if (!entry8(a.p, kUnitsInt + kUnit8Ints * (int)(blockIdx.x / a.p.nkv), entry)) return;
+    const int32_t *u = entry.v;
     const int seq = u[U8_SEQ], block = u[U8_BLOCK], first = u[U8_FIRST], n = u[U8_LEN], row0 = u[U8_ROW];
     const int page = a.p.table[(size_t)seq * a.p.max_blocks + block];
     const bool ok = page >= 0 && page < a.p.n_pages;

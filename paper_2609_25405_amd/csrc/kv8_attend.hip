@@ -16,7 +16,11 @@
 // Tiles (128 pairs of a longer segment): four waves of 32 pairs; 64-key blocks are turned into bf16 once
 // per workgroup on their way into LDS (two buffers, the next block's codes in flight in registers).
 //
-// Long key ranges come as pieces that leave (max, sum, unnormalised output) to a merge launch.
+// Long key ranges come as pieces that leave (max, sum, unnormalised output) to a merge launch.  (Joining
+// them in the workgroup that arrives last was five times slower: its device-scope release and acquire write back and
+// drop the L2 that all other workgroups read through.)
+#include <type_traits>
+
 #include "kv8.hpp"
 
 namespace orthrus {
@@ -42,6 +46,13 @@ __device__ __forceinline__ float quarters_sum(float v) {
     v = p.x + p.y;
     p = partner32(v);
     return p.x + p.y;
+}
+
+// a barrier that orders LDS only: loads from global memory stay in flight across it
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint2 a, uint2 b) { return __builtin_bit_cast(bf16x8, u32x4{a.x, a.y, b.x, b.y}); }
@@ -75,6 +86,11 @@ template <typename T, int NQ> __device__ __forceinline__ void load_q(const T *p,
         const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
         parts_of<NQ>(x, out);
     }
+}
+
+// the sum of a word's two bf16 values and c
+__device__ __forceinline__ float add_pair(uint32_t w, float c) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3f803f80u), c, false);
 }
 
 template <typename T> struct Rows8;
@@ -125,16 +141,69 @@ __device__ void pair_key_by_key(const Attend8 &a, int seq, int head, int pos, in
     l_out = l;
 }
 
+// ------------------------------------------------------------------ pieces of a key range
+template <int HD> __device__ __forceinline__ float *partial_of(const Attend8 &a, int slot, int col) {
+    return a.partials + ((size_t)slot * 16 + col) * (HD + kPartialPad);
+}
+
+// blockIdx.x: merge entry, blockIdx.y: 16 of its (row, head) pairs; the pieces in their order
+template <typename T, int HD> __global__ __launch_bounds__(256) void attend8_merge_kernel(Attend8 a) {
+    constexpr int TPC = 256 / kSmallCols;                 // threads a pair for its factors
+    __shared__ float f[kSmallCols][kMaxPieces + 1], inv[kSmallCols];
+    Entry8<kMerge8Ints> entry;
+    if (!entry8(a.p, a.off_merge + kMerge8Ints * (int)blockIdx.x, entry)) return;
+    const int32_t *me = entry.v;
+    const int n = me[M8_PIECES], slots = me[M8_SLOTS], c0 = blockIdx.y * kSmallCols, tid = threadIdx.x;
+    const int cols = min(kSmallCols, me[M8_LEN] * a.p.group - c0);
+    if (cols <= 0) return;
+    const int slot0 = me[M8_SLOT] + (int)blockIdx.y;
+    {
+        const int col = tid / TPC;
+        float M = -INFINITY, L = 0.f;
+        if (col < cols) {
+            for (int i = tid % TPC; i < n; i += TPC) M = fmaxf(M, partial_of<HD>(a, slot0 + i * slots, col)[0]);
+        }
+#pragma unroll
+        for (int o = 1; o < TPC; o *= 2) M = fmaxf(M, __shfl_xor(M, o, 64));
+        if (col < cols) {
+            for (int i = tid % TPC; i < n; i += TPC) {
+                const float *p = partial_of<HD>(a, slot0 + i * slots, col);
+                // (a piece whose every score was not a number has a sum but no maximum)
+                const float w = p[0] == -INFINITY ? (p[1] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(p[0] - M);
+                f[col][i] = w;
+                L = fmaf(p[1], w, L);
+            }
+        }
+#pragma unroll
+        for (int o = 1; o < TPC; o *= 2) L += __shfl_xor(L, o, 64);
+        if (tid % TPC == 0) inv[col] = L != 0.f ? 1.f / L : 0.f;
+    }
+    __syncthreads();
+    const size_t step = (size_t)slots * 16 * (HD + kPartialPad);
+    for (int u = tid; u < cols * (HD / 4); u += 256) {
+        const int col = u / (HD / 4), d = u % (HD / 4) * 4;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        const float *p = partial_of<HD>(a, slot0, col) + kPartialPad + d;
+#pragma unroll 8
+        for (int i = 0; i < n; ++i) sum += *(const f32x4 *)(p + i * step) * f[col][i];
+        const int c = c0 + col, row = me[M8_ROW] + c / a.p.group, h = me[M8_HEAD] * a.p.group + c % a.p.group;
+        store4((T *)a.out + (size_t)row * a.out_stride + (size_t)h * HD + d, sum[0] * inv[col], sum[1] * inv[col], sum[2] * inv[col],
+               sum[3] * inv[col]);
+    }
+}
+
 // ------------------------------------------------------------------ small items
 template <typename T, int HD, int NW>
-__global__ __launch_bounds__(64 * NW) void attend8_small_kernel(Attend8 a) {
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) void attend8_small_kernel(Attend8 a) {
     using R = Rows8<T>;
     constexpr int QD = HD / 4, KK = HD / 32, DB = HD / 16, STEP = 64, PG = 4;
     constexpr int LD = HD + 4;
-    __shared__ float sm[NW][16], sl[NW][16];
-    __shared__ __attribute__((aligned(16))) float so[NW][16][LD];
-    if (stale8(a.p)) return;
-    const int32_t *it = a.p.meta + a.off_small + kItem8Ints * (int)blockIdx.x;
+    extern __shared__ __attribute__((aligned(16))) char dyn[];
+    float *sm = (float *)dyn, *sl = sm + NW * 16;      // [NW][16] maxima and sums
+    float *so = sl + NW * 16;                          // [NW][pairs][LD] sums
+    Entry8<kItem8Ints> entry;
+    if (!entry8(a.p, a.off_small + kItem8Ints * (int)blockIdx.x, entry)) return;
+    const int32_t *it = entry.v;
     const int seq = it[A8_SEQ], row0 = it[A8_ROW], len = it[A8_LEN], pos0 = it[A8_POS], g = it[A8_HEAD];
     const int key0 = it[A8_KEY0], key1 = it[A8_KEY1], slot = it[A8_SLOT];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -158,23 +227,24 @@ __global__ __launch_bounds__(64 * NW) void attend8_small_kernel(Attend8 a) {
     const int steps = (key1 - key0 + STEP - 1) / STEP;
     u32x4 kr[PG][QD / 16], vr[PG][QD / 16];
     float ks[PG], vs[PG];
-    int valid[PG];
-    auto pages_of = [&](int st, int (&pg)[PG]) {
+    int valid[PG], pg[PG];
+    auto pages_of = [&](int st) {
 #pragma unroll
         for (int p = 0; p < PG; ++p) pg[p] = table[min(key0 / kPage8 + st * PG + p, last)];
     };
     // keys of the step's pages that the item has; bad and absent pages have none and read page 0
-    auto check = [&](int st, int (&pg)[PG]) {
+    int next_valid[PG];
+    auto check = [&](int st) {
 #pragma unroll
         for (int p = 0; p < PG; ++p) {
             const int k = key0 + st * STEP + p * kPage8;
             const bool ok = pg[p] >= 0 && pg[p] < a.p.n_pages;
-            valid[p] = ok ? max(0, min(kPage8, key1 - k)) : 0;
+            next_valid[p] = ok ? max(0, min(kPage8, key1 - k)) : 0;
             if (!ok && k < key1 && lane == 0) flag_error(a.p.err, ORTHRUS_DEVERR_PAGE);
             pg[p] = ok ? pg[p] : 0;
         }
     };
-    auto load = [&](const uint8_t *pool, const float *scales, const int (&pg)[PG], u32x4 (&r)[PG][QD / 16], float (&s)[PG], int at) {
+    auto load = [&](const uint8_t *pool, const float *scales, u32x4 (&r)[PG][QD / 16], float (&s)[PG], int at) {
 #pragma unroll
         for (int p = 0; p < PG; ++p) {
             const size_t head = (size_t)pg[p] * a.p.nkv + g;
@@ -186,15 +256,23 @@ __global__ __launch_bounds__(64 * NW) void attend8_small_kernel(Attend8 a) {
     const int k_at = c * HD + qd * QD;                 // lane (quarter, key): the quarter's dims
     const int v_at = qd * (4 * HD) + c * (HD / 4);     // lane (quarter, dim % 16): 4 slots of every 16th dim
 
+    // the next step's keys are on their way once this step's scores are taken, its values once this
+    // step's are used; its page ids were read a step ahead
+    float ks_next[PG];
+    if (wave < steps) {
+        pages_of(wave);
+        check(wave);
+        load(a.p.k, a.p.ks, kr, ks_next, k_at);
+        load(a.p.v, a.p.vs, vr, vs, v_at);
+        pages_of(min(wave + NW, steps - 1));
+    }
     for (int st = wave; st < steps; st += NW) {
-        int pg[PG];
-        pages_of(st, pg);
-        check(st, pg);
-        load(a.p.k, a.p.ks, pg, kr, ks, k_at);
-        load(a.p.v, a.p.vs, pg, vr, vs, v_at);
+        const bool more = st + NW < steps;
         f32x4 s[PG];
 #pragma unroll
         for (int p = 0; p < PG; ++p) {
+            valid[p] = next_valid[p];
+            ks[p] = ks_next[p];
             s[p] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < KK; ++k) {
@@ -203,6 +281,12 @@ __global__ __launch_bounds__(64 * NW) void attend8_small_kernel(Attend8 a) {
                 for (int n = 0; n < R::NQ; ++n) s[p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[k][n], s[p], 0, 0, 0);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) {
+            check(st + NW);
+            load(a.p.k, a.p.ks, kr, ks_next, k_at);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         const int kbase = key0 + st * STEP;
         float mloc = -INFINITY;
 #pragma unroll
@@ -260,36 +344,44 @@ __global__ __launch_bounds__(64 * NW) void attend8_small_kernel(Attend8 a) {
                 for (int n = 0; n < R::NP; ++n) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], acc[d], 0, 0, 0);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) {
+            load(a.p.v, a.p.vs, vr, vs, v_at);
+            pages_of(min(st + 2 * NW, steps - 1));
+        }
     }
     l = quarters_sum(l);
     if (qd == 0) {
-        sm[wave][c] = m;
-        sl[wave][c] = l;
+        sm[wave * 16 + c] = m;
+        sl[wave * 16 + c] = l;
     }
+    auto sums = [&](int w, int col) { return so + (w * cols + col) * LD; };
+    if (c < cols) {
 #pragma unroll
-    for (int d = 0; d < DB; ++d) *(f32x4 *)&so[wave][c][16 * d + 4 * qd] = acc[d];
+        for (int d = 0; d < DB; ++d) *(f32x4 *)(sums(wave, c) + 16 * d + 4 * qd) = acc[d];
+    }
     __syncthreads();
     // merge the waves in order; four dims a thread
     for (int o = tid; o < cols * (HD / 4); o += 64 * NW) {
         const int col = o / (HD / 4), d = o % (HD / 4) * 4;
         float M = -INFINITY, L = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) M = fmaxf(M, sm[w][col]);
+        for (int w = 0; w < NW; ++w) M = fmaxf(M, sm[w * 16 + col]);
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float f = sm[w][col] == -INFINITY ? (sl[w][col] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(sm[w][col] - M);
-            L += sl[w][col] * f;
-            sum += *(const f32x4 *)&so[w][col][d] * f;
+            const float mw = sm[w * 16 + col], lw = sl[w * 16 + col];
+            const float f = mw == -INFINITY ? (lw == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(mw - M);
+            L += lw * f;
+            sum += *(const f32x4 *)(sums(w, col) + d) * f;
         }
         if (slot >= 0) {
-            float *pp = a.partials + ((size_t)slot * 16 + col) * (HD + 2);
+            float *pp = partial_of<HD>(a, slot, col);
             if (d == 0) {
                 pp[0] = M;
                 pp[1] = L;
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) pp[2 + d + e] = sum[e];
+            *(f32x4 *)(pp + kPartialPad + d) = sum;
         } else {
             const float inv = L != 0.f ? 1.f / L : 0.f;
             T *dst = (T *)a.out + (size_t)(row0 + col / a.p.group) * a.out_stride + (size_t)(g * a.p.group + col % a.p.group) * HD + d;
@@ -297,34 +389,35 @@ __global__ __launch_bounds__(64 * NW) void attend8_small_kernel(Attend8 a) {
         }
     }
     // pairs of an earlier row of several: a later row's key or value that is not finite is masked, not absent
-    if (len == 1) return;
-    __syncthreads();       // after the stores above, which it may replace
-    for (int col = wave; col < cols; col += NW) {
-        float L = 0.f;
-        bool bad = false;
+    if (len > 1) {
+        __syncthreads();       // after the stores above, which it may replace
+        for (int col = wave; col < cols; col += NW) {
+            bool bad = false;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            L += sl[w][col];
-            for (int d = lane; d < HD; d += 64) bad |= !(fabsf(so[w][col][d]) < INFINITY);
-        }
-        if (__ballot(bad) == 0) continue;
-        const int t = col / a.p.group, hh = g * a.p.group + col % a.p.group;
-        float o[HD / 64], mm, ll;
-        pair_key_by_key<T, HD>(a, seq, g, pos0 + t, key0, key1, (const T *)a.q + (size_t)(row0 + t) * a.q_stride + (size_t)hh * HD, mm, ll, o);
-        float *pp = a.partials + ((size_t)max(slot, 0) * 16 + col) * (HD + 2);
-        if (slot >= 0 && lane == 0) {
-            pp[0] = mm;
-            pp[1] = ll;
-        }
+            for (int w = 0; w < NW; ++w)
+                for (int d = lane; d < HD; d += 64) bad |= !(fabsf(sums(w, col)[d]) < INFINITY);
+            if (__ballot(bad) == 0) continue;
+            const int t = col / a.p.group, hh = g * a.p.group + col % a.p.group;
+            if (pos0 + t + 1 >= key1) continue;        // nothing masked
+            float o[HD / 64], mm, ll;
+            pair_key_by_key<T, HD>(a, seq, g, pos0 + t, key0, key1, (const T *)a.q + (size_t)(row0 + t) * a.q_stride + (size_t)hh * HD, mm, ll, o);
+            float *pp = partial_of<HD>(a, max(slot, 0), col);
+            if (slot >= 0 && lane == 0) {
+                pp[0] = mm;
+                pp[1] = ll;
+            }
 #pragma unroll
-        for (int d = 0; d < HD / 64; ++d) {
-            if (slot >= 0) pp[2 + lane + 64 * d] = o[d];
-            else ((T *)a.out)[(size_t)(row0 + t) * a.out_stride + (size_t)hh * HD + lane + 64 * d] = from_f32<T>(ll != 0.f ? o[d] / ll : 0.f);
+            for (int d = 0; d < HD / 64; ++d) {
+                if (slot >= 0) pp[kPartialPad + lane + 64 * d] = o[d];
+                else ((T *)a.out)[(size_t)(row0 + t) * a.out_stride + (size_t)hh * HD + lane + 64 * d] = from_f32<T>(ll != 0.f ? o[d] / ll : 0.f);
+            }
         }
     }
 }
 
 // ------------------------------------------------------------------ tiles of longer segments
+constexpr int kWindow = 256;      // pages
+
 template <int HD> struct Stage8 {
     static constexpr int KEYS = 64, KRB = HD * 2, KCH = KRB / 16;
     static constexpr int KBYTES = KEYS * KRB, VPAGE = HD * kPage8 * 2, BYTES = KBYTES + 4 * VPAGE;
@@ -341,8 +434,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
     constexpr int KS = HD / 16, DB = HD / 32;
     constexpr int KL = HD / 64;              // 16-byte loads of codes a thread and block, keys and values each
     __shared__ __attribute__((aligned(16))) char smem[2 * St::BYTES];
-    if (stale8(a.p)) return;
-    const int32_t *it = a.p.meta + a.off_tiles + kItem8Ints * (int)blockIdx.x;
+    // Page ids (-1: bad) and scales of a run of pages.  Scalar loads would do, but they share a counter with LDS: the barrier
+    // of every step would wait for their memory latency.
+    __shared__ int win_page[kWindow];
+    __shared__ float2 win_scale[kWindow];
+    Entry8<kItem8Ints> entry;
+    if (!entry8(a.p, a.off_tiles + kItem8Ints * (int)blockIdx.x, entry)) return;
+    const int32_t *it = entry.v;
     const int seq = it[A8_SEQ], row0 = it[A8_ROW], len = it[A8_LEN], pos0 = it[A8_POS], g = it[A8_HEAD];
     const int key0 = it[A8_KEY0], key1 = it[A8_KEY1], slot = it[A8_SLOT];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -351,8 +449,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
     const int c = wave * 32 + col, cc = min(c, cols - 1);
     const int tok = cc / a.p.group, h = g * a.p.group + cc % a.p.group;
     const int pos = pos0 + tok;
-    const bool idle = wave * 32 >= cols;                                     // no pairs for this wave
-    const int first_pos = pos0 + min(wave * 32, cols - 1) / a.p.group, last_pos = pos0 + min(wave * 32 + 31, cols - 1) / a.p.group;
+    const int first_pos = pos0 + min(wave * 32, cols - 1) / a.p.group;     // of this wave's pairs
     const int32_t *table = a.p.table + (size_t)seq * a.p.max_blocks;
     const int nkb = (key1 - key0 + St::KEYS - 1) / St::KEYS, last = (key1 - 1) / kPage8;
 
@@ -361,57 +458,78 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
 #pragma unroll
     for (int k = 0; k < KS; ++k) load_q<T, R::NQ>(qp + 16 * k + 8 * half, q[k]);
 
-    // a block's codes: thread (key, part) reads KL x 16 dims of a key; thread (page, quad, 4 lanes of dims) KL x 16
-    // bytes of a page's values
-    u32x4 kr[KL], vr[KL];
-    float ksc, vsc;
-    int kvalid, vvalid;
-    const int krow = tid / 4, kpart = tid % 4;
-    const int vpage = tid / 64, vquad = (tid / 16) % 4, vlane = tid % 16;
-    auto fetch = [&](int b) {
-        const int base = key0 + b * St::KEYS;
-        auto page_of = [&](int p, bool &ok) {
-            const int pg = table[min(base / kPage8 + p, last)];
-            ok = pg >= 0 && pg < a.p.n_pages;
-            if (!ok && base + p * kPage8 < key1 && (tid & 15) == 0) flag_error(a.p.err, ORTHRUS_DEVERR_PAGE);
-            return ok ? pg : 0;
-        };
-        bool ok;
-        size_t head = (size_t)page_of(krow / kPage8, ok) * a.p.nkv + g;
-        kvalid = ok ? 1 : 0;
-        ksc = a.p.ks[head];
-#pragma unroll
-        for (int j = 0; j < KL; ++j) kr[j] = *(const u32x4 *)(a.p.k + head * (kPage8 * HD) + (krow % kPage8) * HD + kpart * (HD / 4) + 16 * j);
-        head = (size_t)page_of(vpage, ok) * a.p.nkv + g;
-        vvalid = ok ? max(0, min(4, key1 - base - vpage * kPage8 - 4 * vquad)) : 0;
-        vsc = a.p.vs[head];
-#pragma unroll
-        for (int j = 0; j < KL; ++j) vr[j] = *(const u32x4 *)(a.p.v + head * (kPage8 * HD) + vquad * (4 * HD) + vlane * (HD / 4) + 16 * j);
+    int w0 = key0 / kPage8;            // first page of the window (a multiple of 4)
+    bool bad = false;
+    auto load_window = [&]() {
+        const int p = w0 + tid;
+        if (p > last) return;
+        const int id = table[p];
+        const bool ok = id >= 0 && id < a.p.n_pages;
+        const size_t head = (size_t)(ok ? id : 0) * a.p.nkv + g;
+        win_page[tid] = ok ? id : -1;
+        win_scale[tid] = ok ? float2{a.p.ks[head], a.p.vs[head]} : float2{1.f, 1.f};
+        if (!ok) flag_error(a.p.err, ORTHRUS_DEVERR_PAGE);
+        bad |= !ok;
     };
-    // as bf16 into buffer buf; what the item does not have is zero
-    auto put = [&](int buf) {
-        char *kl = smem + buf * St::BYTES, *vl = kl + St::KBYTES;
+    static_assert(kWindow == 256, "a page a thread");
+
+    // Wave w takes page w of each block: lane (key, part) reads KL x 16 dims of a key, lane (dim % 16, quad) KL x 16
+    // bytes of the page's values.
+    u32x4 kr[KL], vr[KL];
+    float ksc, vsc, vsc_next;
+    int kvalid, vvalid, page, vpage;        // keys of the page that the item has; pages of the keys' and the values' block
+    const int krow = tid / 4, kpart = tid % 4;
+    const int vquad = lane % 4, vlane = lane / 4;      // (16 lanes then write 128 contiguous bytes of LDS)
+    auto keys_in = [&](int b, int pg) {
+        return pg >= 0 ? max(0, min(kPage8, key1 - (key0 + b * St::KEYS + wave * kPage8))) : 0;
+    };
+    // the keys' page of block b, from the window
+    auto look_up = [&](int b) {
+        const int i = min(key0 / kPage8 + 4 * b + wave, last) - w0;
+        page = __builtin_amdgcn_readfirstlane(win_page[i]);
+        const float2 sc = win_scale[i];
+        ksc = sc.x;
+        vsc_next = sc.y;
+    };
+    // codes of block b's keys (its page looked up), and of the block's values whose keys were fetched before
+    auto fetch_k = [&](int b) {
+        kvalid = keys_in(b, page);
+        const uint8_t *kp = a.p.k + ((size_t)max(page, 0) * a.p.nkv + g) * (kPage8 * HD) + (krow % kPage8) * HD + kpart * (HD / 4);
 #pragma unroll
-        for (int j = 0; j < KL; ++j) {
-            if (!kvalid) kr[j] = u32x4{0u, 0u, 0u, 0u};
-            const float s = kvalid ? ksc : 1.f;
+        for (int j = 0; j < KL; ++j) kr[j] = *(const u32x4 *)(kp + 16 * j);
+    };
+    auto fetch_v = [&](int b) {
+        vvalid = keys_in(b, vpage);
+        const uint8_t *vp = a.p.v + ((size_t)max(vpage, 0) * a.p.nkv + g) * (kPage8 * HD) + vquad * (4 * HD) + vlane * (HD / 4);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint2 lo = word_bf16(kr[j][2 * e], s), hi = word_bf16(kr[j][2 * e + 1], s);
-                const int ch = kpart * (KL * 2) + 2 * j + e;
-                *(u32x4 *)(kl + krow * St::KRB + St::kchunk(krow, ch) * 16) = u32x4{lo.x, lo.y, hi.x, hi.y};
-            }
-        }
-        const uint32_t keep = vvalid == 4 ? 0xffffffffu : (1u << (8 * vvalid)) - 1;
-        const float s = vvalid > 0 ? vsc : 1.f;
-#pragma unroll
-        for (int j = 0; j < KL; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int dim = 16 * (4 * j + e) + vlane;
-                *(uint2 *)(vl + vpage * St::VPAGE + dim * 32 + St::vchunk(dim, vquad / 2) * 16 + (vquad % 2) * 8) =
-                    word_bf16(vr[j][e] & keep, s);
-            }
+        for (int j = 0; j < KL; ++j) vr[j] = *(const u32x4 *)(vp + 16 * j);
+    };
+    auto next_v = [&]() {
+        vpage = page;
+        vsc = vsc_next;
+    };
+
+    // 16-byte chunk i of the thread's keys, word i of its values, as bf16 into buffer buf; what the item does not have
+    // is zero (k_keep, v_keep: masks of the codes, k_mul, v_mul: scales)
+    uint32_t k_keep, v_keep;
+    float k_mul, v_mul;
+    char *const k_dst = smem + krow * St::KRB, *const v_dst = smem + St::KBYTES + wave * St::VPAGE + (vquad % 2) * 8;
+    auto put_k = [&](int buf, int i) {
+        const uint2 lo = word_bf16(kr[i / 2][2 * (i % 2)] & k_keep, k_mul), hi = word_bf16(kr[i / 2][2 * (i % 2) + 1] & k_keep, k_mul);
+        *(u32x4 *)(k_dst + buf * St::BYTES + St::kchunk(krow, kpart * (KL * 2) + i) * 16) = u32x4{lo.x, lo.y, hi.x, hi.y};
+    };
+    auto put_v = [&](int buf, int i) {
+        const int dim = 16 * i + vlane;
+        *(uint2 *)(v_dst + buf * St::BYTES + dim * 32 + St::vchunk(dim, vquad / 2) * 16) = word_bf16(vr[i / 4][i % 4] & v_keep, v_mul);
+    };
+    auto keep_k = [&]() {
+        k_keep = kvalid ? 0xffffffffu : 0u;
+        k_mul = ksc;
+    };
+    auto keep_v = [&]() {
+        const int n = max(0, min(4, vvalid - 4 * vquad));
+        v_keep = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1;
+        v_mul = vsc;
     };
 
     f32x16 acc[DB];
@@ -421,28 +539,21 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
         for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
     float m = -INFINITY, l = 0.f;
 
-    // bit p: page p of the block is bad (its keys are masked; their codes were zeroed)
-    auto compute = [&](int b, uint32_t bad) {
+    // S^T = K Q^T: operand row r holds key r with bits 2 and 3 swapped, so that the eight weights a lane packs for
+    // one page are its slots 8 half .. 8 half + 7
+    const int kcol = col ^ ((((col >> 2) ^ (col >> 3)) & 1) * 12);
+    int k_at[KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) k_at[k] = kcol * St::KRB + St::kchunk(kcol, 2 * k + half) * 16;
+    const int v_at = St::KBYTES + col * 32 + St::vchunk(col, half) * 16;
+    // operand i of the scores (k = i / 2, keys 32 (i % 2) ..) and of the products (page i / DB, dims 32 (i % DB) ..)
+    auto k_frag = [&](int buf, int i) { return *(const bf16x8 *)(smem + buf * St::BYTES + (i % 2) * (32 * St::KRB) + k_at[i / 2]); };
+    auto v_frag = [&](int buf, int i) { return *(const bf16x8 *)(smem + buf * St::BYTES + (i / DB) * St::VPAGE + (i % DB) * 1024 + v_at); };
+    // masks block b's scores and raises the running maximum; bit p of `bad`: page p is bad (its keys are masked,
+    // their codes were zeroed)
+    float neg = 0.f;               // minus the maximum, or zero
+    auto raise = [&](int b, uint32_t bad, f32x16 (&s)[2]) {
         const int base = key0 + b * St::KEYS;
-        if (idle || base > last_pos) return;
-        const char *kl = smem + (b & 1) * St::BYTES, *vl = kl + St::KBYTES;
-        // S^T = K Q^T; operand row r holds key r with bits 2 and 3 swapped, so that the eight weights a lane
-        // packs for one page are its slots 8 half .. 8 half + 7
-        f32x16 s[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[j][e] = 0.f;
-        const int kcol = col ^ ((((col >> 2) ^ (col >> 3)) & 1) * 12);
-#pragma unroll
-        for (int k = 0; k < KS; ++k)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int row = 32 * j + kcol;
-                const bf16x8 kf = *(const bf16x8 *)(kl + row * St::KRB + St::kchunk(row, 2 * k + half) * 16);
-#pragma unroll
-                for (int n = 0; n < R::NQ; ++n) s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[k][n], s[j], 0, 0, 0);
-            }
         if (base + St::KEYS > first_pos || base + St::KEYS > key1 || bad) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
@@ -461,6 +572,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
             const float2 p = partner32(mloc);
             mloc = fmaxf(p.x, p.y) * a.scale;
         }
+        // the maximum follows in jumps of more than 2^8, so that the sums are rarely rescaled
         if (__ballot(mloc > m + 8.f) != 0) {
             const float mn = fmaxf(m, mloc), alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
             l *= alpha;
@@ -469,51 +581,117 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[d][e] *= alpha;
             m = mn;
+            neg = m == -INFINITY ? 0.f : -m;
         }
-        const float neg = m == -INFINITY ? 0.f : -m;
-        bf16x8 pf[2][2][R::NP];
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int k2 = 0; k2 < 2; ++k2) {
-                float x[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    x[e] = __builtin_amdgcn_exp2f(fmaf(s[j][8 * k2 + e], a.scale, neg));
-                    l += x[e];
-                }
-                parts_of<R::NP>(x, pf[j][k2]);
-            }
-        // O^T[dim][pair] += V^T P^T
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const int dim = d * 32 + col;
-                    const bf16x8 vf = *(const bf16x8 *)(vl + (2 * j + k2) * St::VPAGE + dim * 32 + St::vchunk(dim, half) * 16);
-#pragma unroll
-                    for (int n = 0; n < R::NP; ++n) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[j][k2][n], acc[d], 0, 0, 0);
-                }
     };
     auto bad_pages = [&](int b) {
         uint32_t bad = 0;
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const int pg = table[min(key0 / kPage8 + 4 * b + p, last)];
-            if (pg < 0 || pg >= a.p.n_pages) bad |= 1u << p;
+            const int id = table[min(key0 / kPage8 + 4 * b + p, last)];
+            if (id < 0 || id >= a.p.n_pages) bad |= 1u << p;
         }
         return (uint32_t)__builtin_amdgcn_readfirstlane(bad);
     };
 
-    fetch(0);
-    put(0);
-    for (int b = 0; b < nkb; ++b) {
-        __syncthreads();       // block b is whole; everyone is done with block b - 1, whose buffer b + 1 takes
-        if (b + 1 < nkb) fetch(b + 1);
-        compute(b, bad_pages(b));
-        if (b + 1 < nkb) put((b + 1) & 1);
+    load_window();
+    bool any_bad = __syncthreads_or(bad);      // then each block's pages are looked at again
+
+    // Block b's weights run beside block b + 1's scores, and its products beside the next codes' way into LDS (keys one
+    // block ahead of values): the compiler keeps no such order by itself, so every product is a slot with its share of the
+    // vector work, operands read four slots ahead, and nothing moves between slots.
+    constexpr int NA = 2 * KS, NB = 4 * DB, AHEAD = 4, EA = 32 / NA;
+    f32x16 sa[2], sb[2];
+    auto step = [&](int b, auto parity, f32x16 (&s)[2], f32x16 (&next)[2]) {
+        constexpr int P = decltype(parity)::value;           // b % 2
+        bf16x8 ring[AHEAD], pf[4][R::NP];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) ring[i] = k_frag(P ^ 1, i);
+        raise(b, any_bad ? bad_pages(b) : 0, s);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) next[j][e] = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+#pragma unroll
+            for (int n = 0; n < R::NQ; ++n) next[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % AHEAD], q[i / 2][n], next[i % 2], 0, 0, 0);
+            ring[i % AHEAD] = i + AHEAD < NA ? k_frag(P ^ 1, i + AHEAD) : v_frag(P, i + AHEAD - NA);
+#pragma unroll
+            for (int e = EA * i; e < EA * (i + 1); ++e) {
+                s[e / 16][e % 16] = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], a.scale, neg));
+                if (R::NP > 1) l += s[e / 16][e % 16];
+            }
+            if ((EA * (i + 1)) % 8 == 0) {
+                const int t = EA * (i + 1) / 8 - 1;          // page t of the block
+                const float x[8] = {s[t / 2][8 * (t % 2)], s[t / 2][8 * (t % 2) + 1], s[t / 2][8 * (t % 2) + 2], s[t / 2][8 * (t % 2) + 3],
+                                    s[t / 2][8 * (t % 2) + 4], s[t / 2][8 * (t % 2) + 5], s[t / 2][8 * (t % 2) + 6], s[t / 2][8 * (t % 2) + 7]};
+                parts_of<R::NP>(x, pf[t]);
+                if (R::NP == 1) {                            // the sum of the weights as they are used
+                    const u32x4 w = __builtin_bit_cast(u32x4, pf[t][0]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) l = add_pair(w[k], l);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        keep_v();
+        keep_k();
+        next_v();
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+#pragma unroll
+            for (int n = 0; n < R::NP; ++n) acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % AHEAD], pf[i / DB][n], acc[i % DB], 0, 0, 0);
+            if (i + AHEAD < NB) ring[i % AHEAD] = v_frag(P, i + AHEAD);
+            // into the buffers that iteration b - 1 read; the registers take the next ones, most of a step ahead
+            if (i < NB / 2) put_v(P ^ 1, i);
+            else if (i % 2 == 1) put_k(P, (i - NB / 2) / 2);
+            if (i == NB / 2) fetch_v(b + 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (4 * (b + 3) + key0 / kPage8 - w0 >= kWindow && w0 + kWindow <= last) {
+            lds_barrier();
+            w0 += kWindow;
+            load_window();
+            any_bad |= (bool)__syncthreads_or(bad);
+        }
+        look_up(b + 3);
+        fetch_k(b + 3);
+        lds_barrier();
+    };
+    look_up(0);
+    fetch_k(0);
+    next_v();
+    fetch_v(0);
+    keep_k();
+    keep_v();
+#pragma unroll
+    for (int i = 0; i < 2 * KL; ++i) put_k(0, i);
+#pragma unroll
+    for (int i = 0; i < 4 * KL; ++i) put_v(0, i);
+    look_up(1);
+    fetch_k(1);
+    next_v();
+    fetch_v(1);
+    keep_k();
+#pragma unroll
+    for (int i = 0; i < 2 * KL; ++i) put_k(1, i);
+    look_up(2);
+    fetch_k(2);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sa[j][e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int n = 0; n < R::NQ; ++n) sa[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(0, i), q[i / 2][n], sa[i % 2], 0, 0, 0);
+    __syncthreads();
+    for (int b = 0; b < nkb; b += 2) {
+        step(b, std::integral_constant<int, 0>{}, sa, sb);
+        if (b + 1 < nkb) step(b + 1, std::integral_constant<int, 1>{}, sb, sa);
     }
     {
         const float2 p = partner32(l);
@@ -526,86 +704,61 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int e = 0; e < 16; ++e) odd |= !(fabsf(acc[d][e]) < INFINITY);
-    const uint64_t oddb = __ballot(odd && c < cols);
+    const uint64_t oddb = __ballot(odd && c < cols && pos + 1 < key1);     // (a pair that sees every key has nothing masked)
     const uint32_t odd_cols = (uint32_t)oddb | (uint32_t)(oddb >> 32);
     for (int k = 0; k < 32; ++k) {
         if (!(odd_cols >> k & 1)) continue;
         const int ck = wave * 32 + k, t = ck / a.p.group, hh = g * a.p.group + ck % a.p.group;
         float o[HD / 64], mm, ll;
         pair_key_by_key<T, HD>(a, seq, g, pos0 + t, key0, key1, (const T *)a.q + (size_t)(row0 + t) * a.q_stride + (size_t)hh * HD, mm, ll, o);
-        float *pp = a.partials + ((size_t)max(slot, 0) * 16 + ck) * (HD + 2);
+        float *pp = partial_of<HD>(a, max(slot, 0), ck);
         if (slot >= 0 && lane == 0) {
             pp[0] = mm;
             pp[1] = ll;
         }
 #pragma unroll
         for (int d = 0; d < HD / 64; ++d) {
-            if (slot >= 0) pp[2 + lane + 64 * d] = o[d];
+            if (slot >= 0) pp[kPartialPad + lane + 64 * d] = o[d];
             else ((T *)a.out)[(size_t)(row0 + t) * a.out_stride + (size_t)hh * HD + lane + 64 * d] = from_f32<T>(ll != 0.f ? o[d] / ll : 0.f);
         }
     }
-    if (c >= cols || (odd_cols >> col & 1)) return;
-    if (slot >= 0) {
-        float *pp = a.partials + ((size_t)slot * 16 + c) * (HD + 2);
-        if (half == 0) {
-            pp[0] = m;
-            pp[1] = l;
-        }
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float2 *dst = (float2 *)(pp + 2 + d * 32 + k * 8 + half * 4);
-                dst[0] = float2{acc[d][4 * k], acc[d][4 * k + 1]};
-                dst[1] = float2{acc[d][4 * k + 2], acc[d][4 * k + 3]};
+    if (c < cols && !(odd_cols >> col & 1)) {
+        if (slot >= 0) {
+            float *pp = partial_of<HD>(a, slot, c);
+            if (half == 0) {
+                pp[0] = m;
+                pp[1] = l;
             }
-        return;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    *(f32x4 *)(pp + kPartialPad + d * 32 + k * 8 + half * 4) =
+                        f32x4{acc[d][4 * k], acc[d][4 * k + 1], acc[d][4 * k + 2], acc[d][4 * k + 3]};
+        } else {
+            const float inv = l != 0.f ? 1.f / l : 0.f;
+            T *dst = (T *)a.out + (size_t)(row0 + tok) * a.out_stride + (size_t)h * HD;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    store4(dst + d * 32 + k * 8 + half * 4, acc[d][4 * k] * inv, acc[d][4 * k + 1] * inv, acc[d][4 * k + 2] * inv,
+                           acc[d][4 * k + 3] * inv);
+        }
     }
-    const float inv = l != 0.f ? 1.f / l : 0.f;
-    T *dst = (T *)a.out + (size_t)(row0 + tok) * a.out_stride + (size_t)h * HD;
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            store4(dst + d * 32 + k * 8 + half * 4, acc[d][4 * k] * inv, acc[d][4 * k + 1] * inv, acc[d][4 * k + 2] * inv,
-                   acc[d][4 * k + 3] * inv);
 }
 
-// ------------------------------------------------------------------ merge of pieces, in their order
-// blockIdx.x: merge entry, blockIdx.y: eight of its (row, head) pairs, 32 lanes each
-template <typename T, int HD> __global__ __launch_bounds__(256) void attend8_merge_kernel(Attend8 a) {
-    constexpr int N = HD / 32;
-    if (stale8(a.p)) return;
-    const int32_t *me = a.p.meta + a.off_merge + kMerge8Ints * (int)blockIdx.x;
-    const int col = blockIdx.y * 8 + threadIdx.x / 32, d0 = threadIdx.x % 32 * N;
-    if (col >= me[M8_LEN] * a.p.group) return;
-    const int n = me[M8_PIECES];
-    const float *pp = a.partials + ((size_t)me[M8_SLOT] * 16 + col) * (HD + 2);
-    const size_t step = (size_t)me[M8_SLOTS] * 16 * (HD + 2);
-    float M = -INFINITY, L = 0.f, o[N];
-    for (int i = 0; i < n; ++i) M = fmaxf(M, pp[i * step]);
-#pragma unroll
-    for (int d = 0; d < N; ++d) o[d] = 0.f;
-    for (int i = 0; i < n; ++i) {
-        const float *p = pp + i * step;
-        // (a piece whose every score was not a number has a sum but no maximum)
-        const float f = p[0] == -INFINITY ? (p[1] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(p[0] - M);
-        L += p[1] * f;
-#pragma unroll
-        for (int d = 0; d < N; ++d) o[d] += p[2 + d0 + d] * f;
-    }
-    const float inv = L != 0.f ? 1.f / L : 0.f;
-    const int row = me[M8_ROW] + col / a.p.group, h = me[M8_HEAD] * a.p.group + col % a.p.group;
-    T *dst = (T *)a.out + (size_t)row * a.out_stride + (size_t)h * HD + d0;
-#pragma unroll
-    for (int d = 0; d < N; ++d) dst[d] = from_f32<T>(o[d] * inv);
+template <typename T, int HD, int NW> void small_of(const Attend8 &a, hipStream_t s) {
+    const int lds = NW * (32 + a.small_cols * (HD + 4)) * 4;
+    hipLaunchKernelGGL((attend8_small_kernel<T, HD, NW>), dim3(a.n_small), dim3(64 * NW), lds, s, a);
 }
-
 template <typename T, int HD> hipError_t attend_of(const Attend8 &a, hipStream_t s) {
-    if (a.n_small > 0) hipLaunchKernelGGL((attend8_small_kernel<T, HD, 4>), dim3(a.n_small), dim3(256), 0, s, a);
+    if (a.n_small > 0) {
+        if (a.wide && a.small_cols <= 8) small_of<T, HD, 8>(a, s);      // (more pairs' sums would take over 64 KB of LDS)
+        else small_of<T, HD, 4>(a, s);
+    }
     if (a.n_tiles > 0) hipLaunchKernelGGL((attend8_tile_kernel<T, HD>), dim3(a.n_tiles), dim3(256), 0, s, a);
-    if (a.n_merge > 0)
-        hipLaunchKernelGGL((attend8_merge_kernel<T, HD>), dim3(a.n_merge, (a.most_merge_cols + 7) / 8), dim3(256), 0, s, a);
+    if (a.n_merge > 0) hipLaunchKernelGGL((attend8_merge_kernel<T, HD>), dim3(a.n_merge, a.merge_slots), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

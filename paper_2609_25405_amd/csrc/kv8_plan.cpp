@@ -13,10 +13,12 @@ namespace orthrus {
 
 namespace {
 // Key ranges.  An item walks its keys in steps, so one long range can outlast the launch while CUs are
-// idle: ranges longer than twice the launch's mean per workgroup slot are cut into pieces of about
-// that mean, on multiples of kCut keys (a step of a small item's four waves; four of a tile's).
-constexpr int kSlotsSmall = 1024, kSlotsTile = 512, kCut = 256;
-constexpr int kMinPieceSmall = 512, kMinPieceTile = 1024;
+// idle: ranges longer than their share of the launch's workgroup slots are cut into pieces of about that share, on
+// multiples of kCut keys.  A piece costs its partial sums' way through memory, so it has a least length.
+constexpr int kSlotsSmall = 1024, kSlotsTile = 1024, kCut = 64;
+constexpr int kMinPieceSmall = 1024, kMinPieceTile = 1024;
+// few small items run with more waves each (and are cut for a workgroup a CU)
+constexpr int kWideItems = 256;
 
 int64_t piece_keys(int64_t total, int slots, int least) {
     const int64_t mean = (total + slots - 1) / slots;
@@ -49,8 +51,8 @@ void bound_rows8(const orthrus_head_shape &s, int64_t max_rows, int64_t max_segs
     const int64_t units = max_rows / kPage8 + 2 * max_segs;
     const int64_t small = max_segs * nkv, tiles = (max_rows / per_tile + max_segs) * nkv;
     // a range of k keys makes at most min(k / least, pieces allowed) pieces
-    const int64_t ps = std::min<int64_t>(2 * kMaxSmallPieces, small * (max_keys / kMinPieceSmall + 1));
-    const int64_t pt = std::min<int64_t>(2 * kMaxTilePieces, tiles * (max_keys / kMinPieceTile + 1));
+    const int64_t ps = std::min<int64_t>(kMaxSmallPieces, small * (max_keys / kMinPieceSmall + 1));
+    const int64_t pt = std::min<int64_t>(kMaxTilePieces, tiles * (max_keys / kMinPieceTile + 1));
     meta_ints = (size_t)(kUnitsInt + units * kUnit8Ints + (small + ps + tiles + pt) * kItem8Ints + (ps + pt) / 2 * kMerge8Ints);
     slots = (size_t)(ps + pt * (kTileRows8 / kSmallCols));
 }
@@ -92,6 +94,7 @@ int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, co
             t += len;
         }
         const bool few = (int64_t)g.len * group <= kSmallCols;
+        if (few) p.small_cols = std::max(p.small_cols, g.len * group);
         const int step = few ? g.len : per_tile;
         for (int t = 0; t < g.len; t += step) {
             const int len = std::min(step, g.len - t), key1 = g.offset + t + len;
@@ -111,13 +114,13 @@ int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, co
         int pieces = 0;
         std::stable_sort(ranges.begin(), ranges.end(), [](const Range &a, const Range &b) { return a.work > b.work; });
         for (const Range &r : ranges) {
-            int m = r.work > 2 * piece ? (int)((r.work + piece - 1) / piece) : 1;
+            int m = r.work > piece ? (int)std::min<int64_t>(kMaxPieces, (r.work + piece - 1) / piece) : 1;
             if (pieces + m > most_pieces) m = 1;
             int slot = -1;
             if (m > 1) {
                 slot = p.n_slots;
                 merges.push_back({r.row, r.len, r.head, m, slot, slots_each});
-                p.most_merge_cols = std::max(p.most_merge_cols, r.len * group);
+                p.merge_slots = std::max(p.merge_slots, slots_each);
                 p.n_slots += m * slots_each;
                 pieces += m;
             }
@@ -131,8 +134,9 @@ int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, co
         std::stable_sort(items.begin(), items.end(), [](const auto &a, const auto &b) { return a.first > b.first; });
         return items;
     };
-    const auto is = cut(small, piece_keys(keys_small, kSlotsSmall, kMinPieceSmall), 2 * kMaxSmallPieces, 1);
-    const auto it = cut(tiles, piece_keys(keys_tiles, kSlotsTile, kMinPieceTile), 2 * kMaxTilePieces, kTileRows8 / kSmallCols);
+    p.wide = (int)small.size() <= kWideItems;
+    const auto is = cut(small, piece_keys(keys_small, p.wide ? kWideItems : kSlotsSmall, kMinPieceSmall), kMaxSmallPieces, 1);
+    const auto it = cut(tiles, piece_keys(keys_tiles, kSlotsTile, kMinPieceTile), kMaxTilePieces, kTileRows8 / kSmallCols);
     p.n_small = (int)is.size();
     p.n_tiles = (int)it.size();
     p.n_merge = (int)merges.size();

@@ -191,7 +191,7 @@ def test_plans_cover_every_key_once_and_fit_their_workspace(seed):
     covered(shape, segs, counts, items)
     units = sum((o + n - 1) // 16 - o // 16 + 1 for _, o, n in segs)
     meta = (144 + 5 * units + 8 * len(items) + 6 * counts[2]) * 4
-    assert 256 + (meta + 255) // 256 * 256 + counts[3] * 16 * (shape.head_dim + 2) * 4 <= rows.nbytes
+    assert 256 + (meta + 255) // 256 * 256 + counts[3] * 16 * (shape.head_dim + 4) * 4 <= rows.nbytes
 
 
 def test_long_ranges_come_in_pieces_and_short_ones_do_not():
@@ -199,7 +199,7 @@ def test_long_ranges_come_in_pieces_and_short_ones_do_not():
     kv = cpu_cache(shape, 1, 300, 12000)
     rows = cpu_rows(shape, 300, 300, 150000)
     counts, _ = rows.items(kv, [(0, 150000, 1)])
-    assert counts[0] > 256 and counts[2] == 8
+    assert counts[0] >= 256 and counts[2] == 8
     counts, _ = rows.items(kv, [(s, 700, 1) for s in range(300)])
     assert counts[0] == 300 * 8 and counts[2] == counts[3] == 0
     assert rows.items(kv, [])[0] == [0, 0, 0, 0]
