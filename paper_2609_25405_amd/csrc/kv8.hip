@@ -261,6 +261,7 @@ int orthrus_kv8_attend(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t lay
     a.merge_slots = r->plan.merge_slots;
     a.small_cols = r->plan.small_cols;
     a.wide = r->plan.wide;
+    a.joint = r->plan.joint;
     a.off_small = r->plan.off_small;
     a.off_tiles = r->plan.off_tiles;
     a.off_merge = r->plan.off_merge;

@@ -34,7 +34,8 @@ struct RowsPlan {
     int T = 0, n_units = 0, n_small = 0, n_tiles = 0, n_merge = 0, n_slots = 0;
     int merge_slots = 0;                        // slots of a piece, the most of any merge entry
     int small_cols = 0;                         // (row, head) pairs of the largest small item
-    int wide = 0;                               // few small items: more waves each
+    int wide = 0;                               // few small items alone: more waves each
+    int joint = 0;                              // small items behind the tiles in one launch
     int need_seq = 0, need_blocks = 0;          // what a cache must have
     std::vector<int32_t> meta;                  // uploaded verbatim
     int off_small = 0, off_tiles = 0, off_merge = 0;
@@ -90,7 +91,7 @@ struct Attend8 {
     const void *q;
     void *out;
     int64_t q_stride, out_stride;
-    int dtype, n_small, n_tiles, n_merge, merge_slots, small_cols, wide, off_small, off_tiles, off_merge;
+    int dtype, n_small, n_tiles, n_merge, merge_slots, small_cols, wide, joint, off_small, off_tiles, off_merge;
     float scale;             // log2(e) times the softmax scale
     float *partials;
 };
@@ -100,11 +101,10 @@ hipError_t launch_attend8(const Attend8 &a, hipStream_t s);
 // ends.  The entry is read before the comparison, so that the two latencies overlap; in any plan it is in bounds.
 template <int N> struct Entry8 { int32_t v[N]; };
 template <int N> __device__ __forceinline__ bool entry8(const Plan8 &p, int at, Entry8<N> &e) {
+    // (a lane read keeps each load ahead of the branch, and its value in a scalar register)
 #pragma unroll
-    for (int i = 0; i < N; ++i) e.v[i] = p.meta[at + i];
+    for (int i = 0; i < N; ++i) e.v[i] = __builtin_amdgcn_readfirstlane(p.meta[at + i]);
     const int stamp = p.meta[0];
-#pragma unroll
-    for (int i = 0; i < N; ++i) asm volatile("" : "+s"(e.v[i]));       // (the loads stay ahead of the branch)
     if (stamp == p.stamp) return true;
     if (threadIdx.x == 0) flag_error(p.err, ORTHRUS_DEVERR_STALE);
     return false;

@@ -48,6 +48,8 @@ __device__ __forceinline__ float quarters_sum(float v) {
     return p.x + p.y;
 }
 
+__device__ __forceinline__ float first_lane(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
+
 // a barrier that orders LDS only: loads from global memory stay in flight across it
 __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -193,16 +195,17 @@ template <typename T, int HD> __global__ __launch_bounds__(256) void attend8_mer
 }
 
 // ------------------------------------------------------------------ small items
-template <typename T, int HD, int NW>
-__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) void attend8_small_kernel(Attend8 a) {
+// LDS of a small item of `cols` pairs
+template <int HD, int NW> constexpr int small_lds(int cols) { return NW * (32 + cols * (HD + 4)) * 4; }
+
+template <typename T, int HD, int NW> __device__ __forceinline__ void small_item(const Attend8 &a, int index, char *lds) {
     using R = Rows8<T>;
     constexpr int QD = HD / 4, KK = HD / 32, DB = HD / 16, STEP = 64, PG = 4;
     constexpr int LD = HD + 4;
-    extern __shared__ __attribute__((aligned(16))) char dyn[];
-    float *sm = (float *)dyn, *sl = sm + NW * 16;      // [NW][16] maxima and sums
+    float *sm = (float *)lds, *sl = sm + NW * 16;      // [NW][16] maxima and sums
     float *so = sl + NW * 16;                          // [NW][pairs][LD] sums
     Entry8<kItem8Ints> entry;
-    if (!entry8(a.p, a.off_small + kItem8Ints * (int)blockIdx.x, entry)) return;
+    if (!entry8(a.p, a.off_small + kItem8Ints * index, entry)) return;
     const int32_t *it = entry.v;
     const int seq = it[A8_SEQ], row0 = it[A8_ROW], len = it[A8_LEN], pos0 = it[A8_POS], g = it[A8_HEAD];
     const int key0 = it[A8_KEY0], key1 = it[A8_KEY1], slot = it[A8_SLOT];
@@ -427,19 +430,17 @@ template <int HD> struct Stage8 {
     static __device__ __forceinline__ int vchunk(int d, int c) { return c ^ ((d >> 3) & 1); }
 };
 
-template <typename T, int HD>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kernel(Attend8 a) {
+template <typename T, int HD> __device__ __forceinline__ void tile_item(const Attend8 &a, int index, char *smem) {
     using R = Rows8<T>;
     using St = Stage8<HD>;
     constexpr int KS = HD / 16, DB = HD / 32;
     constexpr int KL = HD / 64;              // 16-byte loads of codes a thread and block, keys and values each
-    __shared__ __attribute__((aligned(16))) char smem[2 * St::BYTES];
     // Page ids (-1: bad) and scales of a run of pages.  Scalar loads would do, but they share a counter with LDS: the barrier
     // of every step would wait for their memory latency.
-    __shared__ int win_page[kWindow];
-    __shared__ float2 win_scale[kWindow];
+    float2 *win_scale = (float2 *)(smem + 2 * St::BYTES);
+    int *win_page = (int *)(win_scale + kWindow);
     Entry8<kItem8Ints> entry;
-    if (!entry8(a.p, a.off_tiles + kItem8Ints * (int)blockIdx.x, entry)) return;
+    if (!entry8(a.p, a.off_tiles + kItem8Ints * index, entry)) return;
     const int32_t *it = entry.v;
     const int seq = it[A8_SEQ], row0 = it[A8_ROW], len = it[A8_LEN], pos0 = it[A8_POS], g = it[A8_HEAD];
     const int key0 = it[A8_KEY0], key1 = it[A8_KEY1], slot = it[A8_SLOT];
@@ -483,13 +484,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
     auto keys_in = [&](int b, int pg) {
         return pg >= 0 ? max(0, min(kPage8, key1 - (key0 + b * St::KEYS + wave * kPage8))) : 0;
     };
-    // the keys' page of block b, from the window
+    // the keys' page of block b, from the window: read, and in use
+    int page_read;
+    float2 scale_read;
     auto look_up = [&](int b) {
         const int i = min(key0 / kPage8 + 4 * b + wave, last) - w0;
-        page = __builtin_amdgcn_readfirstlane(win_page[i]);
-        const float2 sc = win_scale[i];
-        ksc = sc.x;
-        vsc_next = sc.y;
+        page_read = win_page[i];
+        scale_read = win_scale[i];
+    };
+    auto use_page = [&]() {
+        page = __builtin_amdgcn_readfirstlane(page_read);
+        ksc = first_lane(scale_read.x);
+        vsc_next = first_lane(scale_read.y);
     };
     // codes of block b's keys (its page looked up), and of the block's values whose keys were fetched before
     auto fetch_k = [&](int b) {
@@ -510,25 +516,33 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
     };
 
     // 16-byte chunk i of the thread's keys, word i of its values, as bf16 into buffer buf; what the item does not have
-    // is zero (k_keep, v_keep: masks of the codes, k_mul, v_mul: scales)
-    uint32_t k_keep, v_keep;
+    // is zero (keep_k, keep_v, once the codes are here)
     float k_mul, v_mul;
-    char *const k_dst = smem + krow * St::KRB, *const v_dst = smem + St::KBYTES + wave * St::VPAGE + (vquad % 2) * 8;
+    const int k_dst = krow * St::KRB + St::kchunk(krow, kpart * (KL * 2)) * 16;      // chunk i enters by exclusive or
+    const int v_dst = St::KBYTES + wave * St::VPAGE + vlane * 32 + St::vchunk(vlane, vquad / 2) * 16 + (vquad % 2) * 8;
     auto put_k = [&](int buf, int i) {
-        const uint2 lo = word_bf16(kr[i / 2][2 * (i % 2)] & k_keep, k_mul), hi = word_bf16(kr[i / 2][2 * (i % 2) + 1] & k_keep, k_mul);
-        *(u32x4 *)(k_dst + buf * St::BYTES + St::kchunk(krow, kpart * (KL * 2) + i) * 16) = u32x4{lo.x, lo.y, hi.x, hi.y};
+        const uint2 lo = word_bf16(kr[i / 2][2 * (i % 2)], k_mul), hi = word_bf16(kr[i / 2][2 * (i % 2) + 1], k_mul);
+        *(u32x4 *)(smem + buf * St::BYTES + (k_dst ^ (i * 16))) = u32x4{lo.x, lo.y, hi.x, hi.y};
     };
     auto put_v = [&](int buf, int i) {
-        const int dim = 16 * i + vlane;
-        *(uint2 *)(v_dst + buf * St::BYTES + dim * 32 + St::vchunk(dim, vquad / 2) * 16) = word_bf16(vr[i / 4][i % 4] & v_keep, v_mul);
+        *(uint2 *)(smem + buf * St::BYTES + i * 512 + v_dst) = word_bf16(vr[i / 4][i % 4], v_mul);       // dim 16 i + vlane
     };
     auto keep_k = [&]() {
-        k_keep = kvalid ? 0xffffffffu : 0u;
-        k_mul = ksc;
+        if (kvalid == 0) {         // (wave-uniform, as the next)
+#pragma unroll
+            for (int j = 0; j < KL; ++j) kr[j] = u32x4{0u, 0u, 0u, 0u};
+        }
     };
     auto keep_v = [&]() {
-        const int n = max(0, min(4, vvalid - 4 * vquad));
-        v_keep = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1;
+        if (vvalid < kPage8) {
+            const int n = max(0, min(4, vvalid - 4 * vquad));
+            const uint32_t keep = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1;
+#pragma unroll
+            for (int j = 0; j < KL; ++j) vr[j] &= keep;
+        }
+    };
+    auto scales = [&]() {
+        k_mul = ksc;
         v_mul = vsc;
     };
 
@@ -542,36 +556,29 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
     // S^T = K Q^T: operand row r holds key r with bits 2 and 3 swapped, so that the eight weights a lane packs for
     // one page are its slots 8 half .. 8 half + 7
     const int kcol = col ^ ((((col >> 2) ^ (col >> 3)) & 1) * 12);
-    int k_at[KS];
-#pragma unroll
-    for (int k = 0; k < KS; ++k) k_at[k] = kcol * St::KRB + St::kchunk(kcol, 2 * k + half) * 16;
+    const int k_at = kcol * St::KRB + St::kchunk(kcol, half) * 16;       // step k's chunk 2 k + half: k enters by exclusive or
     const int v_at = St::KBYTES + col * 32 + St::vchunk(col, half) * 16;
     // operand i of the scores (k = i / 2, keys 32 (i % 2) ..) and of the products (page i / DB, dims 32 (i % DB) ..)
-    auto k_frag = [&](int buf, int i) { return *(const bf16x8 *)(smem + buf * St::BYTES + (i % 2) * (32 * St::KRB) + k_at[i / 2]); };
+    auto k_frag = [&](int buf, int i) { return *(const bf16x8 *)(smem + buf * St::BYTES + (i % 2) * (32 * St::KRB) + (k_at ^ (i / 2 * 32))); };
     auto v_frag = [&](int buf, int i) { return *(const bf16x8 *)(smem + buf * St::BYTES + (i / DB) * St::VPAGE + (i % DB) * 1024 + v_at); };
-    // masks block b's scores and raises the running maximum; bit p of `bad`: page p is bad (its keys are masked,
-    // their codes were zeroed)
+    // masks block b's scores, whose maximum is mx if none is masked, and raises the running maximum; bit p of `bad`:
+    // page p is bad (its keys are masked, their codes were zeroed)
     float neg = 0.f;               // minus the maximum, or zero
-    auto raise = [&](int b, uint32_t bad, f32x16 (&s)[2]) {
+    auto raise = [&](int b, uint32_t bad, f32x16 (&s)[2], float mx) {
         const int base = key0 + b * St::KEYS;
         if (base + St::KEYS > first_pos || base + St::KEYS > key1 || bad) {
+            mx = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int k = 32 * j + (e >> 3) * 16 + half * 8 + ((e >> 2) & 1) * 4 + (e & 3);
                     if (base + k > pos || base + k >= key1 || (bad >> (k / kPage8) & 1)) s[j][e] = -INFINITY;
+                    mx = fmaxf(mx, s[j][e]);
                 }
         }
-        float mloc = s[0][0];
-#pragma unroll
-        for (int e = 1; e < 16; ++e) mloc = fmaxf(mloc, s[0][e]);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) mloc = fmaxf(mloc, s[1][e]);
-        {
-            const float2 p = partner32(mloc);
-            mloc = fmaxf(p.x, p.y) * a.scale;
-        }
+        const float2 p = partner32(mx);
+        const float mloc = fmaxf(p.x, p.y) * a.scale;
         // the maximum follows in jumps of more than 2^8, so that the sums are rarely rescaled
         if (__ballot(mloc > m + 8.f) != 0) {
             const float mn = fmaxf(m, mloc), alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
@@ -599,15 +606,19 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
 
     // Block b's weights run beside block b + 1's scores, and its products beside the next codes' way into LDS (keys one
     // block ahead of values): the compiler keeps no such order by itself, so every product is a slot with its share of the
-    // vector work, operands read four slots ahead, and nothing moves between slots.
-    constexpr int NA = 2 * KS, NB = 4 * DB, AHEAD = 4, EA = 32 / NA;
+    // vector work, operands read three slots ahead, and nothing moves between slots.
+    constexpr int NA = 2 * KS, NB = 4 * DB, AHEAD = 3, EA = 32 / NA, EB = 32 / NB;
     f32x16 sa[2], sb[2];
+    float mx = -INFINITY;          // maximum of the scores at hand
     auto step = [&](int b, auto parity, f32x16 (&s)[2], f32x16 (&next)[2]) {
         constexpr int P = decltype(parity)::value;           // b % 2
         bf16x8 ring[AHEAD], pf[4][R::NP];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) ring[i] = k_frag(P ^ 1, i);
-        raise(b, any_bad ? bad_pages(b) : 0, s);
+        raise(b, any_bad ? bad_pages(b) : 0, s, mx);
+        // (no branch between the slots: the compiler would move their work past it)
+        keep_v();
+        keep_k();
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -636,48 +647,56 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        keep_v();
-        keep_k();
+        scales();
         next_v();
+        mx = -INFINITY;
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
 #pragma unroll
-            for (int n = 0; n < R::NP; ++n) acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % AHEAD], pf[i / DB][n], acc[i % DB], 0, 0, 0);
-            if (i + AHEAD < NB) ring[i % AHEAD] = v_frag(P, i + AHEAD);
+            for (int n = 0; n < R::NP; ++n) acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(NA + i) % AHEAD], pf[i / DB][n], acc[i % DB], 0, 0, 0);
+            if (i + AHEAD < NB) ring[(NA + i) % AHEAD] = v_frag(P, i + AHEAD);
             // into the buffers that iteration b - 1 read; the registers take the next ones, most of a step ahead
             if (i < NB / 2) put_v(P ^ 1, i);
             else if (i % 2 == 1) put_k(P, (i - NB / 2) / 2);
+            if (i == NB / 4) look_up(b + 3);
             if (i == NB / 2) fetch_v(b + 2);
+            if (i == NB - 2) use_page();
+#pragma unroll
+            for (int e = EB * i; e < EB * (i + 1); ++e) mx = fmaxf(mx, next[e / 16][e % 16]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (4 * (b + 3) + key0 / kPage8 - w0 >= kWindow && w0 + kWindow <= last) {
-            lds_barrier();
+        fetch_k(b + 3);
+        if (4 * (b + 4) + key0 / kPage8 - w0 >= kWindow && w0 + kWindow <= last) {
+            lds_barrier();             // everyone has looked up block b + 3
             w0 += kWindow;
             load_window();
             any_bad |= (bool)__syncthreads_or(bad);
         }
-        look_up(b + 3);
-        fetch_k(b + 3);
         lds_barrier();
     };
     look_up(0);
+    use_page();
     fetch_k(0);
     next_v();
     fetch_v(0);
     keep_k();
     keep_v();
+    scales();
 #pragma unroll
     for (int i = 0; i < 2 * KL; ++i) put_k(0, i);
 #pragma unroll
     for (int i = 0; i < 4 * KL; ++i) put_v(0, i);
     look_up(1);
+    use_page();
     fetch_k(1);
     next_v();
     fetch_v(1);
     keep_k();
+    scales();
 #pragma unroll
     for (int i = 0; i < 2 * KL; ++i) put_k(1, i);
     look_up(2);
+    use_page();
     fetch_k(2);
     __syncthreads();
 #pragma unroll
@@ -688,6 +707,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
     for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int n = 0; n < R::NQ; ++n) sa[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(0, i), q[i / 2][n], sa[i % 2], 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, sa[e / 16][e % 16]);
     __syncthreads();
     for (int b = 0; b < nkb; b += 2) {
         step(b, std::integral_constant<int, 0>{}, sa, sb);
@@ -748,16 +769,40 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kern
     }
 }
 
+// ------------------------------------------------------------------ launches
+template <typename T, int HD, int NW>
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) void attend8_small_kernel(Attend8 a) {
+    extern __shared__ __attribute__((aligned(16))) char dyn[];
+    small_item<T, HD, NW>(a, blockIdx.x, dyn);
+}
+
+template <int HD> constexpr int kTileLds = 2 * Stage8<HD>::BYTES + kWindow * 12;
+
+// Tiles, and behind them the small items of a batch that has both: one launch after another left the chip to the tail
+// of the first (2 x 512 rows after 7680 keys beside 14 rows of 2048: 163 us apart, 153 jointly; 64 rows after 512 keys
+// beside 64 rows of 2048: 68 and 53; 256 rows of 4096 beside 4 fresh prompts of 512: 399 and 400).
+template <typename T, int HD, bool SMALL>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kernel(Attend8 a) {
+    __shared__ __attribute__((aligned(16))) char smem[kTileLds<HD>];
+    static_assert(small_lds<HD, 4>(kSmallCols) <= kTileLds<HD>, "a small item's sums");
+    if (!SMALL || (int)blockIdx.x < a.n_tiles) tile_item<T, HD>(a, blockIdx.x, smem);
+    else if constexpr (SMALL) small_item<T, HD, 4>(a, (int)blockIdx.x - a.n_tiles, smem);
+}
+
 template <typename T, int HD, int NW> void small_of(const Attend8 &a, hipStream_t s) {
-    const int lds = NW * (32 + a.small_cols * (HD + 4)) * 4;
+    const int lds = small_lds<HD, NW>(a.small_cols);
     hipLaunchKernelGGL((attend8_small_kernel<T, HD, NW>), dim3(a.n_small), dim3(64 * NW), lds, s, a);
 }
 template <typename T, int HD> hipError_t attend_of(const Attend8 &a, hipStream_t s) {
-    if (a.n_small > 0) {
-        if (a.wide && a.small_cols <= 8) small_of<T, HD, 8>(a, s);      // (more pairs' sums would take over 64 KB of LDS)
-        else small_of<T, HD, 4>(a, s);
+    if (a.joint) {
+        hipLaunchKernelGGL((attend8_tile_kernel<T, HD, true>), dim3(a.n_tiles + a.n_small), dim3(256), 0, s, a);
+    } else {
+        if (a.n_small > 0) {
+            if (a.wide && a.small_cols <= 8) small_of<T, HD, 8>(a, s);      // (more pairs' sums would take over 64 KB of LDS)
+            else small_of<T, HD, 4>(a, s);
+        }
+        if (a.n_tiles > 0) hipLaunchKernelGGL((attend8_tile_kernel<T, HD, false>), dim3(a.n_tiles), dim3(256), 0, s, a);
     }
-    if (a.n_tiles > 0) hipLaunchKernelGGL((attend8_tile_kernel<T, HD>), dim3(a.n_tiles), dim3(256), 0, s, a);
     if (a.n_merge > 0) hipLaunchKernelGGL((attend8_merge_kernel<T, HD>), dim3(a.n_merge, a.merge_slots), dim3(256), 0, s, a);
     return hipGetLastError();
 }

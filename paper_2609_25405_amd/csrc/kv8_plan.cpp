@@ -15,7 +15,7 @@ namespace {
 // Key ranges.  An item walks its keys in steps, so one long range can outlast the launch while CUs are
 // idle: ranges longer than their share of the launch's workgroup slots are cut into pieces of about that share, on
 // multiples of kCut keys.  A piece costs its partial sums' way through memory, so it has a least length.
-constexpr int kSlotsSmall = 1024, kSlotsTile = 1024, kCut = 64;
+constexpr int kSlotsSmall = 1024, kSlotsTile = 512, kCut = 64;
 constexpr int kMinPieceSmall = 1024, kMinPieceTile = 1024;
 // few small items run with more waves each (and are cut for a workgroup a CU)
 constexpr int kWideItems = 256;
@@ -114,7 +114,8 @@ int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, co
         int pieces = 0;
         std::stable_sort(ranges.begin(), ranges.end(), [](const Range &a, const Range &b) { return a.work > b.work; });
         for (const Range &r : ranges) {
-            int m = r.work > piece ? (int)std::min<int64_t>(kMaxPieces, (r.work + piece - 1) / piece) : 1;
+            // (the nearest count: one piece too many for some ranges would be a second round of the launch)
+            int m = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxPieces, (r.work + piece / 2) / piece));
             if (pieces + m > most_pieces) m = 1;
             int slot = -1;
             if (m > 1) {
@@ -134,7 +135,8 @@ int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, co
         std::stable_sort(items.begin(), items.end(), [](const auto &a, const auto &b) { return a.first > b.first; });
         return items;
     };
-    p.wide = (int)small.size() <= kWideItems;
+    p.joint = !small.empty() && !tiles.empty();
+    p.wide = !p.joint && (int)small.size() <= kWideItems;
     const auto is = cut(small, piece_keys(keys_small, p.wide ? kWideItems : kSlotsSmall, kMinPieceSmall), kMaxSmallPieces, 1);
     const auto it = cut(tiles, piece_keys(keys_tiles, kSlotsTile, kMinPieceTile), kMaxTilePieces, kTileRows8 / kSmallCols);
     p.n_small = (int)is.size();
