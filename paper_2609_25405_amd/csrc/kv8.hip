@@ -219,6 +219,7 @@ int orthrus_kv8_append(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t lay
     a.q_out = q_out;
     a.q_stride = q_stride;
     a.n_units = r->plan.n_units;
+    a.most = r->plan.most_unit;
     a.rot = s.rot_dims;
     a.interleaved = s.interleaved;
     a.in_dtype = qkv_dtype;
@@ -235,6 +236,7 @@ int orthrus_kv8_read(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer
     if (r->plan.T == 0) return ORTHRUS_OK;
     if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return ORTHRUS_EINVAL;
     a.n_units = r->plan.n_units;
+    a.most = r->plan.most_unit;
     a.k_out = (bf16 *)k_out;
     a.v_out = (bf16 *)v_out;
     return launch_read8(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;

@@ -32,6 +32,7 @@ constexpr int kTurnsInt = 16, kUnitsInt = kTurnsInt + 128;
 
 struct RowsPlan {
     int T = 0, n_units = 0, n_small = 0, n_tiles = 0, n_merge = 0, n_slots = 0;
+    int most_unit = 0;                          // tokens of the longest unit
     int merge_slots = 0;                        // slots of a piece, the most of any merge entry
     int small_cols = 0;                         // (row, head) pairs of the largest small item
     int wide = 0;                               // few small items alone: more waves each
@@ -74,14 +75,14 @@ struct Append8 {
     const float *q_gain, *k_gain;
     void *q_out;
     int64_t q_stride;
-    int n_units, rot, interleaved, in_dtype, out_dtype;
+    int n_units, most, rot, interleaved, in_dtype, out_dtype;      // most: tokens of the longest unit
     float magnitude, eps;
 };
 hipError_t launch_append8(const Append8 &a, hipStream_t s);
 
 struct Read8 {
     Plan8 p;
-    int n_units;
+    int n_units, most;
     bf16 *k_out, *v_out;
 };
 hipError_t launch_read8(const Read8 &a, hipStream_t s);

@@ -75,16 +75,17 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float ratio) {
     return encode4(lo[0] * ratio, lo[1] * ratio, hi[0] * ratio, hi[1] * ratio);
 }
 
-template <typename TI, typename TO, int HD>
-__global__ __launch_bounds__(256) void append8_kernel(Append8 a) {
+// NT threads serve units of up to N tokens
+template <typename TI, typename TO, int HD, int NT, int N>
+__global__ __launch_bounds__(NT) void append8_kernel(Append8 a) {
     constexpr int LPR = HD / 16;             // lanes of a head row
-    constexpr int GROUPS = 256 / LPR;        // head rows in flight
+    constexpr int GROUPS = NT / LPR;         // head rows in flight
     constexpr int DB = HD / 16;
-    static_assert(GROUPS >= 2 * kPage8, "keys and values of a page in one round");
-    __shared__ float2 turn[kPage8][HD / 2];            // (cos, sin) of each token and pair
-    __shared__ float swap[GROUPS][HD + 4];
-    __shared__ float amax[2][kPage8];
+    static_assert(GROUPS >= 2 * N, "keys and values of a unit in one round");
+    __shared__ float2 turn[N][HD / 2];                 // (cos, sin) of each token and pair
+    __shared__ float amax[2][N];
     __shared__ __attribute__((aligned(16))) uint8_t tile[kPage8 * HD];
+    extern __shared__ __attribute__((aligned(16))) float swap[];       // [GROUPS][HD + 4], where half the pairs meet through it
     const int tid = threadIdx.x, g = blockIdx.x % a.p.nkv;
     Entry8<kUnit8Ints> entry;
     if (!entry8(a.p, kUnitsInt + kUnit8Ints * (int)(blockIdx.x / a.p.nkv), entry)) return;
@@ -94,27 +95,40 @@ __global__ __launch_bounds__(256) void append8_kernel(Append8 a) {
     const bool ok = page >= 0 && page < a.p.n_pages;
     if (!ok && tid == 0) flag_error(a.p.err, ORTHRUS_DEVERR_PAGE);
 
+    const int grp = tid / LPR, i = tid % LPR;
+    // head row `h` of token t: this lane's 16 dims (x[0]: 8 i .., x[1]: HD / 2 + 8 i ..)
+    auto load_row = [&](int t, int h, float (&x)[2][8]) {
+        const TI *src = (const TI *)a.qkv + (size_t)(row0 + t) * a.stride + (size_t)h * HD + 8 * i;
+        load8(src, x[0]);
+        load8(src + HD / 2, x[1]);
+    };
+    // keys and values: group t holds token t's key, group N + t its value; on their way while the angles are taken
+    const int which = grp / N, t = grp % N;      // 0 key, 1 value
+    const bool live = which < 2 && t < n;
+    float x[2][8];
+    if (live) load_row(t, a.p.nq + which * a.p.nkv + g, x);
+    // so are the first round's query heads
+    const int rows = n * a.p.group;
+    float xq[2][8];
+    if (grp < rows) load_row(grp / a.p.group, g * a.p.group + grp % a.p.group, xq);
+
     const int half = a.rot / 2;
     if (half > 0) {
         const double *turns = (const double *)(a.p.meta + kTurnsInt);
-        for (int i = tid; i < n * half; i += 256) {
-            const int t = i / half, pr = i % half;
+        for (int k = tid; k < n * half; k += NT) {
+            const int tk = k / half, pr = k % half;
             // turns modulo one in double: far positions keep their angle
-            const double x = (double)(block * kPage8 + first + t) * turns[pr];
-            const float f = (float)(2.0 * (x - rint(x)));
+            const double c = (double)(block * kPage8 + first + tk) * turns[pr];
+            const float f = (float)(2.0 * (c - rint(c)));
             float sn, cs;
             sincospif(f, &sn, &cs);
-            turn[t][pr] = float2{cs * a.magnitude, sn * a.magnitude};
+            turn[tk][pr] = float2{cs * a.magnitude, sn * a.magnitude};
         }
     }
     __syncthreads();
 
-    const int grp = tid / LPR, i = tid % LPR;
-    // head row `h` of token t, normed and turned, in this lane's 16 dims (x[0]: 8 i .., x[1]: HD / 2 + 8 i ..)
-    auto head_row = [&](int t, int h, const float *gain, bool turns, float (&x)[2][8]) {
-        const TI *src = (const TI *)a.qkv + (size_t)(row0 + t) * a.stride + (size_t)h * HD + 8 * i;
-        load8(src, x[0]);
-        load8(src + HD / 2, x[1]);
+    // norm and turn of a head row
+    auto head_row = [&](int t, const float *gain, bool turns, float (&x)[2][8]) {
         if (gain) {
             float ss = 0.f;
 #pragma unroll
@@ -155,7 +169,7 @@ __global__ __launch_bounds__(256) void append8_kernel(Append8 a) {
             }
         } else {
             // pairs (d, d + rot / 2): the partner's eight dims from another lane of the row
-            float *mine = swap[grp];
+            float *mine = swap + grp * (HD + 4);
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             store8(mine + 8 * i, x[0]);
@@ -181,12 +195,8 @@ __global__ __launch_bounds__(256) void append8_kernel(Append8 a) {
         }
     };
 
-    // keys and values: group t holds token t's key, group 16 + t its value
-    const int which = grp / kPage8, t = grp % kPage8;      // 0 key, 1 value
-    const bool live = which < 2 && t < n;
-    float x[2][8];
     if (live) {
-        head_row(t, which == 0 ? a.p.nq + g : a.p.nq + a.p.nkv + g, which == 0 ? a.k_gain : nullptr, which == 0, x);
+        head_row(t, which == 0 ? a.k_gain : nullptr, which == 0, x);
         float m = 0.f;
 #pragma unroll
         for (int c = 0; c < 2; ++c)
@@ -238,13 +248,14 @@ __global__ __launch_bounds__(256) void append8_kernel(Append8 a) {
     }
     __syncthreads();
     if (ok) {
-        // the values' tile: wave q writes the four slots 4 q .. 4 q + 3; slots outside the unit keep their codes
-        // (rounded again where they came before it and the scale grew)
+        // the values' tile, a wave the four slots 4 q .. 4 q + 3; slots outside the unit keep their codes (rounded again
+        // where they came before it and the scale grew)
         constexpr int W = HD / 64;                         // words a lane
-        const int q = tid / 64, lane = tid % 64;
-        const int lo = max(first - 4 * q, 0), hi = min(first + n - 4 * q, 4);      // new slots of the four
         const bool again_v = scale[1] > was[1];
-        if (hi > 0 && (lo < 4 || again_v)) {
+        const int lane = tid % 64;
+        for (int q = tid / 64; q < 4; q += NT / 64) {
+            const int lo = max(first - 4 * q, 0), hi = min(first + n - 4 * q, 4);      // new slots of the four
+            if (hi <= 0 || (lo >= 4 && !again_v)) continue;
             const uint32_t below = lo >= 4 ? 0xffffffffu : (1u << (8 * lo)) - 1;   // slots before the unit
             const uint32_t fresh = lo >= 4 ? 0u : (hi >= 4 ? 0xffffffffu : (1u << (8 * hi)) - 1) & ~below;
             uint32_t *dst = (uint32_t *)(vp + q * (4 * HD)) + W * lane;
@@ -262,7 +273,7 @@ __global__ __launch_bounds__(256) void append8_kernel(Append8 a) {
         }
         if (scale[0] > was[0]) {
             uint32_t *dst = (uint32_t *)kp;
-            for (int j = tid; j < first * HD / 4; j += 256) dst[j] = rescale4(dst[j], was[0] / scale[0]);
+            for (int j = tid; j < first * HD / 4; j += NT) dst[j] = rescale4(dst[j], was[0] / scale[0]);
         }
         if (tid == 0) {
             a.p.ks[head] = scale[0];
@@ -270,18 +281,25 @@ __global__ __launch_bounds__(256) void append8_kernel(Append8 a) {
         }
     }
 
-    // the query heads of this KV head
-    const int rows = n * a.p.group;
+    // the query heads of this KV head, the next round's on their way while one is turned
     for (int r = grp; r < rows; r += GROUPS) {
-        const int tq = r / a.p.group, h = g * a.p.group + r % a.p.group;
-        head_row(tq, h, a.q_gain, true, x);
+        const int tq = r / a.p.group, h = g * a.p.group + r % a.p.group, rn = r + GROUPS;
+        float next[2][8];
+        if (rn < rows) load_row(rn / a.p.group, g * a.p.group + rn % a.p.group, next);
+        head_row(tq, a.q_gain, true, xq);
         TO *dst = (TO *)a.q_out + (size_t)(row0 + tq) * a.q_stride + (size_t)h * HD + 8 * i;
-        store8(dst, x[0]);
-        store8(dst + HD / 2, x[1]);
+        store8(dst, xq[0]);
+        store8(dst + HD / 2, xq[1]);
+        if (rn < rows) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) xq[c][j] = next[c][j];
+        }
     }
 }
 
-template <int HD> __global__ __launch_bounds__(256) void read8_kernel(Read8 a) {
+template <int HD, int NT> __global__ __launch_bounds__(NT) void read8_kernel(Read8 a) {
     constexpr int PT = HD / 16, DB = HD / 16;              // dims a thread
     __shared__ __attribute__((aligned(16))) uint8_t tile[kPage8 * HD];
     const int tid = threadIdx.x, g = blockIdx.x % a.p.nkv;
@@ -294,54 +312,74 @@ template <int HD> __global__ __launch_bounds__(256) void read8_kernel(Read8 a) {
     if (!ok && tid == 0) flag_error(a.p.err, ORTHRUS_DEVERR_PAGE);
     const size_t head = (size_t)(ok ? page : 0) * a.p.nkv + g;
     const uint8_t *kp = a.p.k + head * (kPage8 * HD), *vp = a.p.v + head * (kPage8 * HD);
-    for (int i = tid; i < kPage8 * HD / 8; i += 256) ((uint2 *)tile)[i] = ((const uint2 *)vp)[i];
+    for (int i = tid; i < kPage8 * HD / 8; i += NT) ((uint2 *)tile)[i] = ((const uint2 *)vp)[i];
     __syncthreads();
-    const int t = tid / 16, slot = first + t, d0 = (tid % 16) * PT;
-    if (t >= n) return;
     const float ks = ok ? a.p.ks[head] : 1.f, vs = ok ? a.p.vs[head] : 1.f;
-    uint32_t ow[2][PT / 2];
+    const int d0 = (tid % 16) * PT;
+    for (int t = tid / 16; t < n; t += NT / 16) {
+        const int slot = first + t;
+        uint32_t ow[2][PT / 2];
 #pragma unroll
-    for (int j = 0; j < PT / 4; ++j) {
-        const uint2 w = word_bf16(ok ? *(const uint32_t *)(kp + slot * HD + d0 + 4 * j) : 0u, ks);
-        ow[0][2 * j] = w.x;
-        ow[0][2 * j + 1] = w.y;
-        uint32_t c = 0;
+        for (int j = 0; j < PT / 4; ++j) {
+            const uint2 w = word_bf16(ok ? *(const uint32_t *)(kp + slot * HD + d0 + 4 * j) : 0u, ks);
+            ow[0][2 * j] = w.x;
+            ow[0][2 * j + 1] = w.y;
+            uint32_t c = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int d = d0 + 4 * j + e;
-            c |= (uint32_t)tile[(slot / 4) * (4 * HD) + (d % 16) * (4 * DB) + (d / 16) * 4 + slot % 4] << (8 * e);
+            for (int e = 0; e < 4; ++e) {
+                const int d = d0 + 4 * j + e;
+                c |= (uint32_t)tile[(slot / 4) * (4 * HD) + (d % 16) * (4 * DB) + (d / 16) * 4 + slot % 4] << (8 * e);
+            }
+            const uint2 v = word_bf16(ok ? c : 0u, vs);
+            ow[1][2 * j] = v.x;
+            ow[1][2 * j + 1] = v.y;
         }
-        const uint2 v = word_bf16(ok ? c : 0u, vs);
-        ow[1][2 * j] = v.x;
-        ow[1][2 * j + 1] = v.y;
-    }
-    const size_t at = (size_t)(row0 + t) * ((size_t)a.p.nkv * HD) + (size_t)g * HD + d0;
+        const size_t at = (size_t)(row0 + t) * ((size_t)a.p.nkv * HD) + (size_t)g * HD + d0;
 #pragma unroll
-    for (int j = 0; j < PT / 4; ++j) {
-        *(uint2 *)(a.k_out + at + 4 * j) = uint2{ow[0][2 * j], ow[0][2 * j + 1]};
-        *(uint2 *)(a.v_out + at + 4 * j) = uint2{ow[1][2 * j], ow[1][2 * j + 1]};
+        for (int j = 0; j < PT / 4; ++j) {
+            *(uint2 *)(a.k_out + at + 4 * j) = uint2{ow[0][2 * j], ow[0][2 * j + 1]};
+            *(uint2 *)(a.v_out + at + 4 * j) = uint2{ow[1][2 * j], ow[1][2 * j + 1]};
+        }
     }
 }
 
-template <typename TI, typename TO> void append_of(const Append8 &a, dim3 grid, hipStream_t s) {
-    if (a.p.hd == 64) hipLaunchKernelGGL((append8_kernel<TI, TO, 64>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((append8_kernel<TI, TO, 128>), grid, dim3(256), 0, s, a);
+// Units of a few tokens (decode rows) take one wave each: four would mostly wait (256 rows over 8 KV heads 10.4 us with 256
+// threads a unit).
+constexpr int kFewTokens = 4;
+
+template <typename TI, typename TO, int HD, int NT, int N> void append_of(const Append8 &a, hipStream_t s) {
+    // half pairs of a head that turns in part meet through LDS, in NT / (HD / 16) rows
+    const int lds = !a.interleaved && a.rot > 0 && a.rot < HD ? NT / (HD / 16) * (HD + 4) * 4 : 0;
+    hipLaunchKernelGGL((append8_kernel<TI, TO, HD, NT, N>), dim3(a.n_units * a.p.nkv), dim3(NT), lds, s, a);
+}
+template <typename TI, typename TO, int HD> void append_of(const Append8 &a, hipStream_t s) {
+    if (a.most <= kFewTokens) append_of<TI, TO, HD, 64, kFewTokens>(a, s);
+    else append_of<TI, TO, HD, 256, kPage8>(a, s);
+}
+template <int HD> void append_of(const Append8 &a, hipStream_t s) {
+    if (a.in_dtype == ORTHRUS_BF16) append_of<bf16, bf16, HD>(a, s);
+    else if (a.out_dtype == ORTHRUS_BF16) append_of<float, bf16, HD>(a, s);
+    else append_of<float, float, HD>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_append8(const Append8 &a, hipStream_t s) {
-    const dim3 grid(a.n_units * a.p.nkv);
-    if (a.in_dtype == ORTHRUS_BF16) append_of<bf16, bf16>(a, grid, s);
-    else if (a.out_dtype == ORTHRUS_BF16) append_of<float, bf16>(a, grid, s);
-    else append_of<float, float>(a, grid, s);
+    if (a.p.hd == 64) append_of<64>(a, s);
+    else append_of<128>(a, s);
     return hipGetLastError();
 }
 
 hipError_t launch_read8(const Read8 &a, hipStream_t s) {
     const dim3 grid(a.n_units * a.p.nkv);
-    if (a.p.hd == 64) hipLaunchKernelGGL(read8_kernel<64>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(read8_kernel<128>, grid, dim3(256), 0, s, a);
+    const bool few = a.most <= kFewTokens;
+    if (a.p.hd == 64) {
+        if (few) hipLaunchKernelGGL((read8_kernel<64, 64>), grid, dim3(64), 0, s, a);
+        else hipLaunchKernelGGL((read8_kernel<64, 256>), grid, dim3(256), 0, s, a);
+    } else {
+        if (few) hipLaunchKernelGGL((read8_kernel<128, 64>), grid, dim3(64), 0, s, a);
+        else hipLaunchKernelGGL((read8_kernel<128, 256>), grid, dim3(256), 0, s, a);
+    }
     return hipGetLastError();
 }
 

@@ -14,11 +14,17 @@ namespace orthrus {
 namespace {
 // Key ranges.  An item walks its keys in steps, so one long range can outlast the launch while CUs are
 // idle: ranges longer than their share of the launch's workgroup slots are cut into pieces of about that share, on
-// multiples of kCut keys.  A piece costs its partial sums' way through memory, so it has a least length.
-constexpr int kSlotsSmall = 1024, kSlotsTile = 512, kCut = 64;
-constexpr int kMinPieceSmall = 1024, kMinPieceTile = 1024;
-// few small items run with more waves each (and are cut for a workgroup a CU)
-constexpr int kWideItems = 256;
+// multiples of kCut keys.  A piece costs its partial sums' way through memory and, with the others, a merge launch of
+// about 5 us, so it has a least length.
+constexpr int kCut = 64;
+// Small items run three workgroups of four waves a CU (64 rows of 2560 keys over 8 KV heads 60 us; cut for 1024 slots
+// 66, for 512 60; contexts of 1024 to 4096 61, 64 and 67 us).
+constexpr int kSlotsSmall = 768, kMinPieceSmall = 1024;
+// Few of them run with eight waves each, cut for fewer workgroups (one row of 4000 keys over 8 KV heads 12.5 us in
+// pieces of at least 512 keys, 14.5 of 1024; 16 rows of 2000 17.6 us in 192 slots, 18.8 in 256, 21.9 in 384).
+constexpr int kWideItems = 256, kSlotsWide = 192, kMinPieceWide = 512;
+// Tiles run two workgroups a CU.
+constexpr int kSlotsTile = 512, kMinPieceTile = 1024;
 
 int64_t piece_keys(int64_t total, int slots, int least) {
     const int64_t mean = (total + slots - 1) / slots;
@@ -51,7 +57,7 @@ void bound_rows8(const orthrus_head_shape &s, int64_t max_rows, int64_t max_segs
     const int64_t units = max_rows / kPage8 + 2 * max_segs;
     const int64_t small = max_segs * nkv, tiles = (max_rows / per_tile + max_segs) * nkv;
     // a range of k keys makes at most min(k / least, pieces allowed) pieces
-    const int64_t ps = std::min<int64_t>(kMaxSmallPieces, small * (max_keys / kMinPieceSmall + 1));
+    const int64_t ps = std::min<int64_t>(kMaxSmallPieces, small * (max_keys / kMinPieceWide + 1));
     const int64_t pt = std::min<int64_t>(kMaxTilePieces, tiles * (max_keys / kMinPieceTile + 1));
     meta_ints = (size_t)(kUnitsInt + units * kUnit8Ints + (small + ps + tiles + pt) * kItem8Ints + (ps + pt) / 2 * kMerge8Ints);
     slots = (size_t)(ps + pt * (kTileRows8 / kSmallCols));
@@ -90,6 +96,7 @@ int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, co
         const orthrus_segment &g = seg[i];
         for (int t = 0; t < g.len;) {
             const int pos = g.offset + t, first = pos % kPage8, len = std::min(kPage8 - first, g.len - t);
+            p.most_unit = std::max(p.most_unit, len);
             units.insert(units.end(), {g.seq, pos / kPage8, first, len, row + t});
             t += len;
         }
@@ -137,7 +144,7 @@ int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, co
     };
     p.joint = !small.empty() && !tiles.empty();
     p.wide = !p.joint && (int)small.size() <= kWideItems;
-    const auto is = cut(small, piece_keys(keys_small, p.wide ? kWideItems : kSlotsSmall, kMinPieceSmall), kMaxSmallPieces, 1);
+    const auto is = cut(small, p.wide ? piece_keys(keys_small, kSlotsWide, kMinPieceWide) : piece_keys(keys_small, kSlotsSmall, kMinPieceSmall), kMaxSmallPieces, 1);
     const auto it = cut(tiles, piece_keys(keys_tiles, kSlotsTile, kMinPieceTile), kMaxTilePieces, kTileRows8 / kSmallCols);
     p.n_small = (int)is.size();
     p.n_tiles = (int)it.size();
