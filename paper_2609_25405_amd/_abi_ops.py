@@ -38,6 +38,9 @@ SIGNATURES = {
     "orthrus_kv8_read": (c_int, [c_void_p, POINTER(orthrus_kv8), c_int32, c_void_p, c_void_p, c_void_p]),
     "orthrus_kv8_attend": (c_int, [c_void_p, POINTER(orthrus_kv8), c_int32, c_void_p, c_int64, c_float, c_void_p, c_int64,
                                    c_void_p]),
+    "orthrus_step_kv8_bytes": (c_size_t, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32]),
+    "orthrus_step_kv8": (c_int, [c_void_p, c_void_p, POINTER(_abi.orthrus_batch), POINTER(orthrus_kv8), POINTER(orthrus_kv8),
+                                 c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
     "orthrus_logprobs_bytes": (c_size_t, [c_int32, c_int32, c_int32]),
     "orthrus_logprobs": (c_int, [c_void_p, c_int64, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
                                  c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),

@@ -30,6 +30,7 @@ struct orthrus_rows {
     bool planned = false;
     int device = -1, stamp = 0;
     char *ws = nullptr;
+    int *err = nullptr;            // device error word
     // pinned staging, double-buffered; an event marks when a buffer's upload is done
     void *stage[2] = {nullptr, nullptr}, *stage_dev[2] = {nullptr, nullptr};
     size_t stage_bytes[2] = {0, 0};
@@ -64,7 +65,7 @@ int plan_args(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer, Plan8
     const size_t heads = (size_t)kv->n_pages * s.n_kv_heads, bytes = heads * kPage8 * s.head_dim;
     p.meta = (const int32_t *)(r->ws + kPlanOffset);
     p.stamp = r->stamp;
-    p.err = (int *)r->ws;
+    p.err = r->err;
     p.k = (uint8_t *)kv->k_cache + layer * bytes;
     p.v = (uint8_t *)kv->v_cache + layer * bytes;
     p.ks = kv->k_scale + layer * heads;
@@ -84,6 +85,62 @@ bool rows_ok(const void *base, int64_t stride, int64_t least) {
 }
 
 }  // namespace
+
+namespace orthrus {
+
+int rows_prepare(const orthrus_rows *r, const orthrus_kv8 *kv, const orthrus_segment *segments, int n, RowsPlan &p, size_t &bytes) {
+    if (!r || !kv8_ok(kv)) return ORTHRUS_EINVAL;
+    try {
+        const int rc = plan_rows8(r->shape, r->turns, *kv, segments, n, p);
+        if (rc) return rc;
+        const size_t meta = up256(p.meta.size() * 4);
+        p.meta.resize(meta / 4, 0);
+        bytes = kPlanOffset + meta + (size_t)p.n_slots * kSmallCols * (r->shape.head_dim + kPartialPad) * 4;
+    } catch (...) {
+        return ORTHRUS_ECAPACITY;   // out of host memory
+    }
+    return ORTHRUS_OK;
+}
+
+int rows_upload(orthrus_rows *r, RowsPlan &&p, void *workspace, int *err, void *stream) {
+    hipStream_t s = (hipStream_t)stream;
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    HIP_TRY(hipStreamIsCapturing(s, &cap));
+    if (cap != hipStreamCaptureStatusNone) return ORTHRUS_EUNSUPPORTED;
+    int dev = -1;
+    HIP_TRY(hipGetDevice(&dev));
+    if (r->device >= 0 && dev != r->device) return ORTHRUS_EINVAL;
+    r->device = dev;
+    const size_t meta = p.meta.size() * 4;
+    const int stamp = next_stamp.fetch_add(1);
+    p.meta[0] = stamp;
+    const int i = r->next;
+    if (r->ev[i]) HIP_TRY(hipEventSynchronize(r->ev[i]));
+    else HIP_TRY(hipEventCreateWithFlags(&r->ev[i], hipEventDisableTiming));
+    if (r->stage_bytes[i] < meta) {
+        if (r->stage[i]) (void)hipHostFree(r->stage[i]);   // its last upload is done
+        r->stage[i] = r->stage_dev[i] = nullptr;
+        r->stage_bytes[i] = 0;
+        HIP_TRY(hipHostMalloc(&r->stage[i], 2 * meta, hipHostMallocCoherent));
+        HIP_TRY(hipHostGetDevicePointer(&r->stage_dev[i], r->stage[i], 0));
+        r->stage_bytes[i] = 2 * meta;
+    }
+    std::memcpy(r->stage[i], p.meta.data(), meta);
+    const int n16 = (int)(meta / 16), blocks = std::min((n16 + 255) / 256, 128);
+    hipLaunchKernelGGL(plan_upload_kernel, dim3(blocks), dim3(256), 0, s, (const int4 *)r->stage_dev[i],
+                       (int4 *)((char *)workspace + kPlanOffset), n16);
+    HIP_TRY(hipGetLastError());
+    HIP_TRY(hipEventRecord(r->ev[i], s));
+    r->next ^= 1;
+    r->plan = std::move(p);
+    r->stamp = stamp;
+    r->ws = (char *)workspace;
+    r->err = err;
+    r->planned = true;
+    return ORTHRUS_OK;
+}
+
+}  // namespace orthrus
 
 extern "C" {
 
@@ -153,50 +210,13 @@ int orthrus_rows_items(const orthrus_rows *r, const orthrus_kv8 *kv, const orthr
 
 int orthrus_rows_plan(orthrus_rows *r, const orthrus_kv8 *kv, const orthrus_segment *segments, int32_t n, void *workspace,
                       size_t ws_bytes, void *stream) {
-    if (!r || !kv8_ok(kv) || !workspace || ((uintptr_t)workspace & 255)) return ORTHRUS_EINVAL;
-    try {
-        RowsPlan p;
-        const int rc = plan_rows8(r->shape, r->turns, *kv, segments, n, p);
-        if (rc) return rc;
-        const size_t meta = up256(p.meta.size() * 4);
-        if (ws_bytes < kPlanOffset + meta + (size_t)p.n_slots * kSmallCols * (r->shape.head_dim + kPartialPad) * 4) return ORTHRUS_ECAPACITY;
-        hipStream_t s = (hipStream_t)stream;
-        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-        HIP_TRY(hipStreamIsCapturing(s, &cap));
-        if (cap != hipStreamCaptureStatusNone) return ORTHRUS_EUNSUPPORTED;
-        int dev = -1;
-        HIP_TRY(hipGetDevice(&dev));
-        if (r->device >= 0 && dev != r->device) return ORTHRUS_EINVAL;
-        r->device = dev;
-        p.meta.resize(meta / 4, 0);
-        const int stamp = next_stamp.fetch_add(1);
-        p.meta[0] = stamp;
-        const int i = r->next;
-        if (r->ev[i]) HIP_TRY(hipEventSynchronize(r->ev[i]));
-        else HIP_TRY(hipEventCreateWithFlags(&r->ev[i], hipEventDisableTiming));
-        if (r->stage_bytes[i] < meta) {
-            if (r->stage[i]) (void)hipHostFree(r->stage[i]);   // its last upload is done
-            r->stage[i] = r->stage_dev[i] = nullptr;
-            r->stage_bytes[i] = 0;
-            HIP_TRY(hipHostMalloc(&r->stage[i], 2 * meta, hipHostMallocCoherent));
-            HIP_TRY(hipHostGetDevicePointer(&r->stage_dev[i], r->stage[i], 0));
-            r->stage_bytes[i] = 2 * meta;
-        }
-        std::memcpy(r->stage[i], p.meta.data(), meta);
-        const int n16 = (int)(meta / 16), blocks = std::min((n16 + 255) / 256, 128);
-        hipLaunchKernelGGL(plan_upload_kernel, dim3(blocks), dim3(256), 0, s, (const int4 *)r->stage_dev[i],
-                           (int4 *)((char *)workspace + kPlanOffset), n16);
-        HIP_TRY(hipGetLastError());
-        HIP_TRY(hipEventRecord(r->ev[i], s));
-        r->next ^= 1;
-        r->plan = std::move(p);
-        r->stamp = stamp;
-        r->ws = (char *)workspace;
-        r->planned = true;
-    } catch (...) {
-        return ORTHRUS_ECAPACITY;   // out of host memory
-    }
-    return ORTHRUS_OK;
+    if (!workspace || ((uintptr_t)workspace & 255)) return ORTHRUS_EINVAL;
+    RowsPlan p;
+    size_t bytes = 0;
+    const int rc = rows_prepare(r, kv, segments, n, p, bytes);
+    if (rc) return rc;
+    if (ws_bytes < bytes) return ORTHRUS_ECAPACITY;
+    return rows_upload(r, std::move(p), workspace, (int *)workspace, stream);
 }
 
 int orthrus_kv8_append(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer, const void *qkv, int32_t qkv_dtype,

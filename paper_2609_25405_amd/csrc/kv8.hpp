@@ -45,6 +45,10 @@ struct RowsPlan {
 int validate_shape8(const orthrus_head_shape &s);
 int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, const orthrus_kv8 &kv,
                const orthrus_segment *seg, int n, RowsPlan &out);
+// The two halves of planning: validate and plan on the host (which also gives the workspace bytes that it takes), then
+// upload.  err: the device error word that the plan's kernels flag.
+int rows_prepare(const orthrus_rows *r, const orthrus_kv8 *kv, const orthrus_segment *segments, int n, RowsPlan &p, size_t &bytes);
+int rows_upload(orthrus_rows *r, RowsPlan &&p, void *workspace, int *err, void *stream);
 // most meta ints and partial slots that a plan of these sizes can have
 void bound_rows8(const orthrus_head_shape &s, int64_t max_rows, int64_t max_segs, int64_t max_keys, size_t &meta_ints, size_t &slots);
 

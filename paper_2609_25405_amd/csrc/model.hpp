@@ -8,6 +8,7 @@
 #include <string>
 #include <vector>
 
+#include "orthrus/kv8.h"
 #include "plan.hpp"
 
 struct orthrus_model : public orthrus::Model {
@@ -28,6 +29,10 @@ struct orthrus_model : public orthrus::Model {
     hipStream_t aux = nullptr;
     hipEvent_t ev_fork = nullptr, ev_join = nullptr;
     std::mutex step_mu;
+    // steps through an 8-bit cache (orthrus_step_kv8): the plans of the embedding model's and of the generator's rows,
+    // made on first use; kv8_mu serialises the host side of such steps
+    std::mutex kv8_mu;
+    orthrus_rows *rows8[2] = {nullptr, nullptr};
     // kernel timing (orthrus_profile_begin / _end); prof_only (orthrus_profile_only) limits the
     // timed launches to one name, empty = all
     bool profiling = false;

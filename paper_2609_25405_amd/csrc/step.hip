@@ -14,6 +14,7 @@
 
 #include "common.hpp"
 #include "gemm_skinny.hpp"
+#include "kv8.hpp"
 #include "model.hpp"
 #include "orthrus.h"
 #include "plan.hpp"
@@ -258,6 +259,7 @@ void orthrus_model_destroy(orthrus_model *m) {
     }
     if (m->ev_fork) (void)hipEventDestroy(m->ev_fork);
     if (m->ev_join) (void)hipEventDestroy(m->ev_join);
+    for (orthrus_rows *r : m->rows8) orthrus_rows_destroy(r);
     delete m;
 }
 
@@ -308,13 +310,49 @@ int orthrus_plan(const orthrus_model *emb, const orthrus_model *gen, const orthr
 namespace orthrus {
 namespace {
 
-// One step (the body of orthrus_step).  no_alloc (orthrus_step_noalloc): the metadata is copied
+// The rows and cache of a step through an 8-bit cache: one part for all rows that share a model and a cache, else the
+// embedding model's and the generator's.
+struct Step8 {
+    const orthrus_kv8 *kv[2];              // embedding, generator
+    struct Part { orthrus_rows *rows; const orthrus_kv8 *kv; int r0; RowsPlan plan; size_t bytes; } part[2];
+    int n_parts = 0;
+};
+
+int plan_step8(const orthrus_model *emb, const orthrus_model *gen, const orthrus_batch &b, const StepPlan &p, Step8 &k8) {
+    orthrus_model *mh = const_cast<orthrus_model *>(emb);
+    const orthrus_config &c = emb->cfg;
+    std::vector<orthrus_segment> seg[2];
+    for (int i = 0; i < b.n_chunks; ++i) seg[0].push_back({b.chunks[i].seq, b.chunks[i].offset, b.chunks[i].len});
+    const bool one = emb == gen && p.shared_kv;
+    std::vector<orthrus_segment> &g = seg[one ? 0 : 1];
+    for (int i = 0; i < b.n_gen_chunks; ++i) g.push_back({b.gen_chunks[i].seq, b.gen_chunks[i].offset, b.gen_chunks[i].len});
+    for (int i = 0; i < b.n_decode; ++i) g.push_back({b.rows[i].seq, b.rows[i].ctx_len, 1});
+    for (int i = 0; i < 2; ++i) {
+        if (seg[i].empty()) continue;
+        if (!mh->rows8[i]) {
+            const orthrus_head_shape s{c.n_q_heads, c.n_kv_heads, c.head_dim, c.page_size, c.dtype, c.head_dim, 0, c.rope_base, 1.f, 0.f, nullptr};
+            const int rc = orthrus_rows_create(&s, &mh->rows8[i]);
+            if (rc) return rc;
+        }
+        Step8::Part &part = k8.part[k8.n_parts++];
+        part.rows = mh->rows8[i];
+        part.kv = k8.kv[i];
+        part.r0 = i == 0 ? 0 : p.Te;
+        const int rc = rows_prepare(part.rows, part.kv, seg[i].data(), (int)seg[i].size(), part.plan, part.bytes);
+        if (rc) return rc;
+    }
+    return ORTHRUS_OK;
+}
+
+// One step (the body of orthrus_step; with k8, of orthrus_step_kv8).  no_alloc
+// (orthrus_step_noalloc): the metadata is copied
 // with hipMemcpyAsync from host memory together with a zero error word, both row groups run on
 // `stream` (no auxiliary stream, no events) and kernel timing is off, so nothing is allocated
 // or created.
 int step_impl(const orthrus_model *emb, const orthrus_model *gen, const orthrus_batch *batch,
               const orthrus_kv *emb_kv, const orthrus_kv *gen_kv, float *acc_sum, float *acc_w,
-              float *out_logits, float *out_emb, void *workspace, size_t ws_bytes, void *stream, bool no_alloc) {
+              float *out_logits, float *out_emb, void *workspace, size_t ws_bytes, void *stream, bool no_alloc,
+              Step8 *k8 = nullptr) {
     if (!emb || !gen || !batch || !workspace || !kv_ok(emb_kv, emb) || !kv_ok(gen_kv, gen)) return ORTHRUS_EINVAL;
     if (gen != emb && !same_shape(emb->cfg, gen->cfg)) return ORTHRUS_EUNSUPPORTED;
     if (batch->n_chunks > 0 && (!acc_sum || !acc_w || !out_emb)) return ORTHRUS_EINVAL;
@@ -327,7 +365,13 @@ int step_impl(const orthrus_model *emb, const orthrus_model *gen, const orthrus_
     const Model &M = *emb;
     const orthrus_config &c = M.cfg;
     const Layout L = make_layout(M, p.T, p.meta.size(), p.n_partials);
-    if (ws_bytes < L.total) return ORTHRUS_ECAPACITY;
+    size_t total = L.total;
+    if (k8) {
+        rc = plan_step8(emb, gen, *batch, p, *k8);
+        if (rc) return rc;
+        for (int i = 0; i < k8->n_parts; ++i) total += up(k8->part[i].bytes);
+    }
+    if (ws_bytes < total) return ORTHRUS_ECAPACITY;
 
     hipStream_t s = (hipStream_t)stream;
     Prof prof{no_alloc ? nullptr : const_cast<orthrus_model *>(emb), s};
@@ -353,6 +397,14 @@ int step_impl(const orthrus_model *emb, const orthrus_model *gen, const orthrus_
     char *ws = (char *)workspace;
     int *err = (int *)(ws + L.err);
     const int32_t *meta = (const int32_t *)(ws + L.meta);
+    if (k8) {
+        size_t at = L.total;               // the rows' plans behind the step's own layout
+        for (int i = 0; i < k8->n_parts; ++i) {
+            rc = rows_upload(k8->part[i].rows, std::move(k8->part[i].plan), ws + at, err, stream);
+            if (rc) return rc;
+            at += up(k8->part[i].bytes);
+        }
+    }
     if (no_alloc) {
         // [error word region (zeros) | metadata] in one copy: every call starts with no error bits
         static_assert(sizeof(int32_t) == 4, "int32 metadata");
@@ -424,7 +476,7 @@ int step_impl(const orthrus_model *emb, const orthrus_model *gen, const orthrus_
 
     // split-K slabs of the last residual-add projection, not yet added to x
     float *slabs = dt == ORTHRUS_BF16 ? (float *)(ws + L.split_slabs) : nullptr;
-    float2 *rope_cs = dt == ORTHRUS_BF16 ? (float2 *)(ws + L.rope_cs) : nullptr;
+    float2 *rope_cs = dt == ORTHRUS_BF16 && !k8 ? (float2 *)(ws + L.rope_cs) : nullptr;
     const size_t slab_stride = (size_t)T * d;
     int pending = 0;
     auto norm = [&](bool gather, const Group &g, const float *gain) -> hipError_t {
@@ -638,12 +690,32 @@ int step_impl(const orthrus_model *emb, const orthrus_model *gen, const orthrus_
         return combine ? launch_attn_combine(dt, ag, n_dec, groups[gi].st) : launch_attention(dt, ag, groups[gi].st);
     };
 
+    // an 8-bit cache: rotation, append and attention of layer l, part by part on its group's stream.  The append takes
+    // whole fp32 rows, so the projection's variants that rotate or leave slabs behind are not used.
+    auto rows8 = [&](int l) -> int {
+        for (int i = 0; i < k8->n_parts; ++i) {
+            const Step8::Part &part = k8->part[i];
+            const Group &g = groups[n_groups == 2 ? (part.r0 == groups[1].r0 ? 1 : 0) : 0];
+            int r = timed(g.st, prof.on() ? std::string("kv8_append") + g.tag : std::string(), [&]() {
+                return orthrus_kv8_append(part.rows, part.kv, l, qkv + (size_t)part.r0 * qkvd, ORTHRUS_F32, qkvd, nullptr, nullptr,
+                                          qb + (size_t)part.r0 * qd * es, qd, g.st) == ORTHRUS_OK ? hipSuccess : hipErrorUnknown;
+            });
+            if (r) return r;
+            r = timed(g.st, prof.on() ? std::string("kv8_attend") + g.tag : std::string(), [&]() {
+                return orthrus_kv8_attend(part.rows, part.kv, l, qb + (size_t)part.r0 * qd * es, qd, 0.f,
+                                          ob + (size_t)part.r0 * qd * es, qd, g.st) == ORTHRUS_OK ? hipSuccess : hipErrorUnknown;
+            });
+            if (r) return r;
+        }
+        return ORTHRUS_OK;
+    };
+
     // Projections of gemm_skinny.hip (bf16, no adapters, every row group of few rows):
     // they finish their rows themselves (residual add, rotation and append), so no slabs of
     // theirs are pending, and where no other projection's are and it pays they also norm the rows of x
     const bool few = dt == ORTHRUS_BF16 && p.n_used == 0;
     auto skinny = [&](int N, int K) { return few && skinny_takes(max_rows, N, K); };
-    const bool sk_qkv = few && skinny_takes_qkv(max_rows, qkvd, d), sk_o = skinny(d, qd), sk_gu = skinny(2 * F, d), sk_down = skinny(d, F);
+    const bool sk_qkv = few && !k8 && skinny_takes_qkv(max_rows, qkvd, d), sk_o = skinny(d, qd), sk_gu = skinny(2 * F, d), sk_down = skinny(d, F);
     auto skinny_args = [&](const Group &g, const void *A, int lda, const void *B0, int N, int K) {
         SkinnyArgs sa{};
         sa.A = (const char *)A + (size_t)g.r0 * lda * es;
@@ -677,7 +749,7 @@ int step_impl(const orthrus_model *emb, const orthrus_model *gen, const orthrus_
         ra.v_cache[0] = (char *)emb_kv->v_cache + l * e_stride;
         ra.k_cache[1] = (char *)gen_kv->k_cache + l * g_stride;
         ra.v_cache[1] = (char *)gen_kv->v_cache + l * g_stride;
-        const int qkv_splits = dt == ORTHRUS_BF16 && (size_t)kQkvSplits * T <= qkv_slab_rows(T)
+        const int qkv_splits = dt == ORTHRUS_BF16 && !k8 && (size_t)kQkvSplits * T <= qkv_slab_rows(T)
                                    ? gemm_qkv_splits(max_rows, qkvd, d, shared_chip)
                                    : 1;
         if (sk_qkv) {
@@ -722,7 +794,9 @@ int step_impl(const orthrus_model *emb, const orthrus_model *gen, const orthrus_
                 RUNG(groups[gi], "gemm_qkv", gemm(EPI_STORE_F32, groups[gi], act, d, lw.w_qkv, nullptr, qkv, qkvd, 4, qkvd, d, lg));
             }
             ra.nslab = 1;
-            if (n_groups == 2) {
+            if (k8) {
+                SYNC_GROUPS(rows8(l));
+            } else if (n_groups == 2) {
                 for (int gi = 0; gi < n_groups; ++gi) RUNG(groups[gi], "rope_append", rope_group(groups[gi]));
             } else {
                 RUN("rope_append", launch_rope_append(dt, ra, s));
@@ -732,7 +806,9 @@ int step_impl(const orthrus_model *emb, const orthrus_model *gen, const orthrus_
             aa.k_cache[i] = ra.k_cache[i];
             aa.v_cache[i] = ra.v_cache[i];
         }
-        if (n_groups == 2) {
+        if (k8) {
+            // rows8 ran the attention too
+        } else if (n_groups == 2) {
             RUNG(groups[0], "attention", attn_group(0, false));
             if (p.n_merge_emb > 0) RUNG(groups[0], "attn_combine", attn_group(0, true));
             RUNG(groups[1], "attention", attn_group(1, false));
@@ -907,6 +983,48 @@ int orthrus_step(const orthrus_model *emb, const orthrus_model *gen, const orthr
                  float *out_logits, float *out_emb, void *workspace, size_t ws_bytes, void *stream) {
     return step_impl(emb, gen, batch, emb_kv, gen_kv, acc_sum, acc_w, out_logits, out_emb, workspace, ws_bytes,
                      stream, false);
+}
+
+size_t orthrus_step_kv8_bytes(const orthrus_model *emb, const orthrus_model *gen, int32_t max_tokens, int32_t max_chunks,
+                              int32_t max_decode, int32_t max_ctx) {
+    const size_t own = orthrus_workspace_bytes(emb, gen, max_tokens, max_chunks, max_decode, max_ctx);
+    if (own == 0) return 0;
+    const orthrus_config &c = emb->cfg;
+    const orthrus_head_shape s{c.n_q_heads, c.n_kv_heads, c.head_dim, c.page_size, c.dtype, c.head_dim, 0, c.rope_base, 1.f, 0.f, nullptr};
+    size_t bytes = own;
+    // two parts may each hold most of the rows; a chunk sees at most its end, a decode row its context and itself
+    const int64_t segs = (int64_t)max_chunks + max_decode, keys = (int64_t)max_ctx + max_tokens;
+    for (int i = 0; i < 2; ++i) {
+        size_t ints = 0, slots = 0;
+        bound_rows8(s, max_tokens, segs, keys, ints, slots);
+        bytes += up(kPlanOffset + up(ints * 4) + slots * kSmallCols * (size_t)(c.head_dim + kPartialPad) * 4);
+    }
+    return bytes;
+}
+
+int orthrus_step_kv8(const orthrus_model *emb, const orthrus_model *gen, const orthrus_batch *batch, const orthrus_kv8 *emb_kv,
+                     const orthrus_kv8 *gen_kv, float *acc_sum, float *acc_w, float *out_logits, float *out_emb, void *workspace,
+                     size_t ws_bytes, void *stream) {
+    if (!emb || !gen || !emb_kv || !gen_kv || ((uintptr_t)workspace & 255)) return ORTHRUS_EINVAL;
+    Step8 k8{};
+    orthrus_kv kv[2];
+    for (int i = 0; i < 2; ++i) {
+        const orthrus_kv8 *k = i == 0 ? emb_kv : gen_kv;
+        k8.kv[i] = k;
+        kv[i] = orthrus_kv{k->k_cache, k->v_cache, k->block_table, k->n_pages, k->n_seq, k->max_blocks};
+        if (k->n_layers < emb->cfg.n_layers) return ORTHRUS_EINVAL;
+    }
+    // one cache or two: pools, scales, tables and sizes are all the same, or no pool or scale is
+    const orthrus_kv8 &e = *emb_kv, &g = *gen_kv;
+    const bool same = e.k_cache == g.k_cache;
+    if (same ? std::memcmp(&e, &g, sizeof e) != 0
+             : e.v_cache == g.v_cache || e.k_scale == g.k_scale || e.v_scale == g.v_scale) return ORTHRUS_EINVAL;
+    try {
+        std::lock_guard<std::mutex> lk(const_cast<orthrus_model *>(emb)->kv8_mu);
+        return step_impl(emb, gen, batch, &kv[0], &kv[1], acc_sum, acc_w, out_logits, out_emb, workspace, ws_bytes, stream, false, &k8);
+    } catch (...) {
+        return ORTHRUS_ECAPACITY;   // out of host memory
+    }
 }
 
 int orthrus_step_noalloc(const orthrus_model *emb, const orthrus_model *gen, const orthrus_batch *batch,

@@ -15,6 +15,7 @@ import torch
 
 from . import _abi as A
 from . import _abi_ops as O
+from . import runtime as R
 from .runtime import current_stream
 
 PAGE = 16
@@ -253,6 +254,37 @@ def kv8_attend(rows: RaggedRows, kv: DeviceKV8, layer: int, q: torch.Tensor, out
     stride, out_stride = rows._rows_of(q, width, s.torch_dtype, "q"), rows._rows_of(out, width, s.torch_dtype, "out")
     _check(O.load().orthrus_kv8_attend(rows.handle, kv._ref, layer, q.data_ptr(), stride, scale or 0.0, out.data_ptr(), out_stride,
                                        _stream(stream, dev)), "orthrus_kv8_attend")
+
+
+class WorkspaceKV8(R.Workspace):
+    """Workspace of `step_kv8` (sizes as those of runtime.Workspace; a chunk's end counts as a context)."""
+
+    def __init__(self, emb: R.DeviceModel, gen: R.DeviceModel, max_tokens: int, max_chunks: int, max_decode: int, max_ctx: int,
+                 device="cuda"):
+        self.nbytes = int(O.load().orthrus_step_kv8_bytes(emb.handle, gen.handle, max_tokens, max_chunks, max_decode, max_ctx))
+        if self.nbytes == 0:
+            raise A.OrthrusError(A.ORTHRUS_EINVAL, "orthrus_step_kv8_bytes")
+        self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+        _here(self.buf)
+        _check(A.orthrus_workspace_init(_ptr(self.buf), _stream(None)), "orthrus_workspace_init")
+
+
+def step_kv8(emb: R.DeviceModel, gen: R.DeviceModel, batch, emb_kv: DeviceKV8, gen_kv: DeviceKV8, acc_sum: torch.Tensor,
+             acc_w: torch.Tensor, out_logits: Optional[torch.Tensor], out_emb: Optional[torch.Tensor], ws: WorkspaceKV8,
+             stream: Optional[int] = None, packed: Optional[R.PackedBatch] = None, hidden: Optional[torch.Tensor] = None) -> None:
+    """One mixed step through 8-bit caches (orthrus_step_kv8): arguments as those of runtime.step."""
+    dev = _here(ws.buf, acc_sum, acc_w, out_logits, out_emb, hidden)
+    pb = packed if packed is not None else R.PackedBatch(batch)
+    for kv, m in ((emb_kv, emb), (gen_kv, gen)):
+        kv._on(dev)
+        _need((kv.shape.n_kv_heads, kv.shape.head_dim) == (m.cfg.n_kv_heads, m.cfg.head_dim), "cache of other heads")
+    if hidden is not None:
+        _need(hidden.dtype == torch.float32 and hidden.is_contiguous() and hidden.dim() == 3 and
+              hidden.shape[0] >= emb_kv.n_seq and hidden.shape[1:] == (pb.c.hidden_stride, emb.cfg.d_model), "hidden buffer shape")
+        pb.c.hidden = hidden.data_ptr()
+    rc = O.load().orthrus_step_kv8(emb.handle, gen.handle, byref(pb.c), emb_kv._ref, gen_kv._ref, _ptr(acc_sum), _ptr(acc_w),
+                                   _ptr(out_logits), _ptr(out_emb), _ptr(ws.buf), ws.nbytes, _stream(stream, dev))
+    _check(rc, "orthrus_step_kv8")
 
 
 def logprobs_workspace(rows: int, vocab: int, n_top: int = 0, device="cuda") -> Optional[torch.Tensor]:

@@ -247,3 +247,53 @@ def test_scores_definition():
     p = np.exp(x - 3) / np.exp(x - 3).sum()
     assert rank == 1 and ids.tolist() == [1, 3, 0] and math.isclose(lp, math.log(p[3]))
     assert math.isclose(ent, -sum(v * math.log(v) for v in p if v > 0)) and np.allclose(tops, np.log(p[[1, 3, 0]]))
+
+
+def test_step_refusals():
+    """orthrus_step_kv8 turns away what it cannot run before it touches a device."""
+    from paper_2609_25405_amd import runtime as R
+    from workload import Batch, DecodeRow, EmbChunk, draw_tokens, make_weights, tiny_config
+    cfg = tiny_config("bf16")
+    m = R.DeviceModel(cfg, make_weights(cfg, 1), device="cpu")
+    shape = ops.HeadShape(4, 4, 64)
+    kv = ops.DeviceKV8(shape, 2, 40, 6, 4, device="cpu")
+    other = ops.DeviceKV8(shape, 2, 40, 6, 4, device="cpu")
+    b = Batch([EmbChunk(0, 0, 5, True)], [DecodeRow(1, 9)], draw_tokens(1, 0, 6, cfg.vocab))
+    n = O.load().orthrus_step_kv8_bytes(m.handle, m.handle, 6, 1, 1, 9)
+    assert n > A.orthrus_workspace_bytes(m.handle, m.handle, 6, 1, 1, 9)
+    assert O.load().orthrus_step_kv8_bytes(None, m.handle, 6, 1, 1, 9) == 0
+    assert O.load().orthrus_step_kv8_bytes(m.handle, m.handle, 6, -1, 1, 9) == 0
+    buf = torch.zeros(4096, dtype=torch.uint8)
+    at = -(-buf.data_ptr() // 256) * 256
+    out = torch.zeros(6, max(cfg.vocab, cfg.d_model))
+
+    def call(e, g, ws=at, size=2048, batch=b):
+        p = R.PackedBatch(batch)
+        return O.load().orthrus_step_kv8(m.handle, m.handle, ctypes.byref(p.c), e and ctypes.byref(e), g and ctypes.byref(g),
+                                         out.data_ptr(), out.data_ptr(), out.data_ptr(), out.data_ptr(), ws, size, None)
+
+    def changed(**kw):
+        s = kv.struct()
+        for k, v in kw.items():
+            setattr(s, k, v)
+        return s
+
+    good = kv.struct()
+    assert call(good, good) == A.ORTHRUS_ECAPACITY                    # the workspace is too small: all else is in order
+    assert call(good, kv.struct()) == A.ORTHRUS_ECAPACITY             # the same cache named twice
+    assert call(good, other.struct()) == A.ORTHRUS_ECAPACITY
+    assert call(None, good) == call(good, None) == A.ORTHRUS_EINVAL
+    assert call(good, good, ws=at + 16) == call(good, good, ws=None) == A.ORTHRUS_EINVAL
+    few = changed(n_layers=1)
+    assert call(few, few) == A.ORTHRUS_EINVAL
+    for kw in (dict(n_pages=39), dict(block_table=other.block_table.data_ptr()), dict(v_scale=other.v_scale.data_ptr()),
+               dict(k_cache=other.k.data_ptr())):
+        assert call(good, changed(**kw)) == A.ORTHRUS_EINVAL, kw
+    for kw in (dict(k_scale=None), dict(v_cache=None), dict(k_cache=kv.k.data_ptr() + 4)):
+        bad = changed(**kw)
+        assert call(bad, bad) == A.ORTHRUS_EINVAL, kw
+    twice = Batch([EmbChunk(1, 0, 5, True)], [DecodeRow(1, 9)], draw_tokens(1, 0, 6, cfg.vocab))
+    assert call(good, good, batch=twice) == A.ORTHRUS_EDUPSEQ
+    assert call(good, other.struct(), batch=twice) == A.ORTHRUS_ECAPACITY
+    long = Batch([], [DecodeRow(1, 64)], draw_tokens(1, 0, 1, cfg.vocab))
+    assert call(good, good, batch=long) == A.ORTHRUS_ECAPACITY
