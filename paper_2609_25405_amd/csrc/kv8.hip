@@ -140,6 +140,36 @@ int rows_upload(orthrus_rows *r, RowsPlan &&p, void *workspace, int *err, void *
     return ORTHRUS_OK;
 }
 
+int append_rows8(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer, const void *qkv, int32_t qkv_dtype, int64_t row_stride,
+                 int64_t slab, const float *q_gain, const float *k_gain, void *q_out, int64_t q_stride, void *stream) {
+    Append8 a{};
+    const int rc = plan_args(r, kv, layer, a.p);
+    if (rc) return rc;
+    const orthrus_head_shape &s = r->shape;
+    if (qkv_dtype != ORTHRUS_F32 && qkv_dtype != ORTHRUS_BF16) return ORTHRUS_EINVAL;
+    if (qkv_dtype == ORTHRUS_BF16 && s.dtype != ORTHRUS_BF16) return ORTHRUS_EUNSUPPORTED;
+    if (r->plan.T == 0) return ORTHRUS_OK;
+    const int64_t q_dim = (int64_t)s.n_q_heads * s.head_dim;
+    if (!rows_ok(qkv, row_stride, q_dim + 2 * (int64_t)s.n_kv_heads * s.head_dim) || !rows_ok(q_out, q_stride, q_dim)) return ORTHRUS_EINVAL;
+    if (!aligned16(q_gain) || !aligned16(k_gain)) return ORTHRUS_EINVAL;
+    a.qkv = qkv;
+    a.stride = row_stride;
+    a.slab = slab;
+    a.q_gain = q_gain;
+    a.k_gain = k_gain;
+    a.q_out = q_out;
+    a.q_stride = q_stride;
+    a.n_units = r->plan.n_units;
+    a.most = r->plan.most_unit;
+    a.rot = s.rot_dims;
+    a.interleaved = s.interleaved;
+    a.in_dtype = qkv_dtype;
+    a.out_dtype = s.dtype;
+    a.magnitude = s.rope_magnitude;
+    a.eps = s.norm_eps;
+    return launch_append8(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
+}
+
 }  // namespace orthrus
 
 extern "C" {
@@ -222,31 +252,7 @@ int orthrus_rows_plan(orthrus_rows *r, const orthrus_kv8 *kv, const orthrus_segm
 int orthrus_kv8_append(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer, const void *qkv, int32_t qkv_dtype,
                        int64_t row_stride, const float *q_gain, const float *k_gain, void *q_out, int64_t q_stride,
                        void *stream) {
-    Append8 a{};
-    const int rc = plan_args(r, kv, layer, a.p);
-    if (rc) return rc;
-    const orthrus_head_shape &s = r->shape;
-    if (qkv_dtype != ORTHRUS_F32 && qkv_dtype != ORTHRUS_BF16) return ORTHRUS_EINVAL;
-    if (qkv_dtype == ORTHRUS_BF16 && s.dtype != ORTHRUS_BF16) return ORTHRUS_EUNSUPPORTED;
-    if (r->plan.T == 0) return ORTHRUS_OK;
-    const int64_t q_dim = (int64_t)s.n_q_heads * s.head_dim;
-    if (!rows_ok(qkv, row_stride, q_dim + 2 * (int64_t)s.n_kv_heads * s.head_dim) || !rows_ok(q_out, q_stride, q_dim)) return ORTHRUS_EINVAL;
-    if (!aligned16(q_gain) || !aligned16(k_gain)) return ORTHRUS_EINVAL;
-    a.qkv = qkv;
-    a.stride = row_stride;
-    a.q_gain = q_gain;
-    a.k_gain = k_gain;
-    a.q_out = q_out;
-    a.q_stride = q_stride;
-    a.n_units = r->plan.n_units;
-    a.most = r->plan.most_unit;
-    a.rot = s.rot_dims;
-    a.interleaved = s.interleaved;
-    a.in_dtype = qkv_dtype;
-    a.out_dtype = s.dtype;
-    a.magnitude = s.rope_magnitude;
-    a.eps = s.norm_eps;
-    return launch_append8(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
+    return append_rows8(r, kv, layer, qkv, qkv_dtype, row_stride, 0, q_gain, k_gain, q_out, q_stride, stream);
 }
 
 int orthrus_kv8_read(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer, void *k_out, void *v_out, void *stream) {

@@ -49,6 +49,9 @@ int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, co
 // upload.  err: the device error word that the plan's kernels flag.
 int rows_prepare(const orthrus_rows *r, const orthrus_kv8 *kv, const orthrus_segment *segments, int n, RowsPlan &p, size_t &bytes);
 int rows_upload(orthrus_rows *r, RowsPlan &&p, void *workspace, int *err, void *stream);
+// orthrus_kv8_append of fp32 rows that come in two parts, `slab` elements apart (0: one part)
+int append_rows8(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer, const void *qkv, int32_t qkv_dtype, int64_t row_stride,
+                 int64_t slab, const float *q_gain, const float *k_gain, void *q_out, int64_t q_stride, void *stream);
 // most meta ints and partial slots that a plan of these sizes can have
 void bound_rows8(const orthrus_head_shape &s, int64_t max_rows, int64_t max_segs, int64_t max_keys, size_t &meta_ints, size_t &slots);
 
@@ -76,6 +79,7 @@ struct Append8 {
     Plan8 p;
     const void *qkv;
     int64_t stride;
+    int64_t slab;            // elements to a second part of the rows (fp32), to be added; 0: none
     const float *q_gain, *k_gain;
     void *q_out;
     int64_t q_stride;

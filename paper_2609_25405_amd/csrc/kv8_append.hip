@@ -9,6 +9,8 @@
 // A head row of HD dims lies over HD / 16 lanes; lane i holds dims 8 i .. 8 i + 7 and HD / 2 + 8 i ..
 // + 7, two 16-byte loads of bf16, so that the pairs (i, i + HD / 2) of a head that turns whole, and
 // the pairs (2 i, 2 i + 1), are in one lane; pairs of a head that turns in part meet through LDS.
+#include <type_traits>
+
 #include "kv8.hpp"
 
 namespace orthrus {
@@ -101,6 +103,17 @@ __global__ __launch_bounds__(NT) void append8_kernel(Append8 a) {
         const TI *src = (const TI *)a.qkv + (size_t)(row0 + t) * a.stride + (size_t)h * HD + 8 * i;
         load8(src, x[0]);
         load8(src + HD / 2, x[1]);
+        if constexpr (std::is_same<TI, float>::value) {
+            if (a.slab) {                      // a projection in two parts: their sum
+                float y[2][8];
+                load8(src + a.slab, y[0]);
+                load8(src + a.slab + HD / 2, y[1]);
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[c][j] += y[c][j];
+            }
+        }
     };
     // keys and values: group t holds token t's key, group N + t its value; on their way while the angles are taken
     const int which = grp / N, t = grp % N;      // 0 key, 1 value

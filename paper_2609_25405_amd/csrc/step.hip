@@ -36,7 +36,7 @@ constexpr int kMaxSplits = 4;
 // 64x128 or 128x128 tiles that rotate and append themselves) was slower at every size: 7B shape, 64
 // rows 42.6 us against 18.6 + 6.9, 544 rows 59 against 33 + 11, 2048-wide shape 370 rows 28
 // against 14 + 7.  Partial sums of at most kQkvSplitRows rows fit the region of qkv_slab_rows(T).
-constexpr int kQkvSplits = 2;
+constexpr int kQkvSplits = 2;   // the 8-bit append adds at most two parts
 constexpr int kQkvSplitRows = 2560;
 size_t qkv_slab_rows(size_t T) { return (size_t)kQkvSplits * std::min<size_t>(T, kQkvSplitRows); }
 
@@ -690,15 +690,15 @@ int step_impl(const orthrus_model *emb, const orthrus_model *gen, const orthrus_
         return combine ? launch_attn_combine(dt, ag, n_dec, groups[gi].st) : launch_attention(dt, ag, groups[gi].st);
     };
 
-    // an 8-bit cache: rotation, append and attention of layer l, part by part on its group's stream.  The append takes
-    // whole fp32 rows, so the projection's variants that rotate or leave slabs behind are not used.
-    auto rows8 = [&](int l) -> int {
+    // an 8-bit cache: rotation, append and attention of layer l, part by part on its group's stream; `slab`:
+    // elements between the projection's two parts (0: one).  The projection that rotates its rows itself is not used.
+    auto rows8 = [&](int l, int64_t slab) -> int {
         for (int i = 0; i < k8->n_parts; ++i) {
             const Step8::Part &part = k8->part[i];
             const Group &g = groups[n_groups == 2 ? (part.r0 == groups[1].r0 ? 1 : 0) : 0];
             int r = timed(g.st, prof.on() ? std::string("kv8_append") + g.tag : std::string(), [&]() {
-                return orthrus_kv8_append(part.rows, part.kv, l, qkv + (size_t)part.r0 * qkvd, ORTHRUS_F32, qkvd, nullptr, nullptr,
-                                          qb + (size_t)part.r0 * qd * es, qd, g.st) == ORTHRUS_OK ? hipSuccess : hipErrorUnknown;
+                return append_rows8(part.rows, part.kv, l, qkv + (size_t)part.r0 * qkvd, ORTHRUS_F32, qkvd, slab, nullptr, nullptr,
+                                    qb + (size_t)part.r0 * qd * es, qd, g.st) == ORTHRUS_OK ? hipSuccess : hipErrorUnknown;
             });
             if (r) return r;
             r = timed(g.st, prof.on() ? std::string("kv8_attend") + g.tag : std::string(), [&]() {
@@ -749,7 +749,7 @@ int step_impl(const orthrus_model *emb, const orthrus_model *gen, const orthrus_
         ra.v_cache[0] = (char *)emb_kv->v_cache + l * e_stride;
         ra.k_cache[1] = (char *)gen_kv->k_cache + l * g_stride;
         ra.v_cache[1] = (char *)gen_kv->v_cache + l * g_stride;
-        const int qkv_splits = dt == ORTHRUS_BF16 && !k8 && (size_t)kQkvSplits * T <= qkv_slab_rows(T)
+        const int qkv_splits = dt == ORTHRUS_BF16 && (size_t)kQkvSplits * T <= qkv_slab_rows(T)
                                    ? gemm_qkv_splits(max_rows, qkvd, d, shared_chip)
                                    : 1;
         if (sk_qkv) {
@@ -781,7 +781,9 @@ int step_impl(const orthrus_model *emb, const orthrus_model *gen, const orthrus_
             }
             ra.nslab = qkv_splits;
             ra.slab_stride = (size_t)T * qkvd;
-            if (n_groups == 2) {
+            if (k8) {
+                SYNC_GROUPS(rows8(l, (int64_t)T * qkvd));
+            } else if (n_groups == 2) {
                 for (int gi = 0; gi < n_groups; ++gi) RUNG(groups[gi], "rope_append", rope_group(groups[gi]));
             } else {
                 RUN("rope_append", launch_rope_append(dt, ra, s));
@@ -795,7 +797,7 @@ int step_impl(const orthrus_model *emb, const orthrus_model *gen, const orthrus_
             }
             ra.nslab = 1;
             if (k8) {
-                SYNC_GROUPS(rows8(l));
+                SYNC_GROUPS(rows8(l, 0));
             } else if (n_groups == 2) {
                 for (int gi = 0; gi < n_groups; ++gi) RUNG(groups[gi], "rope_append", rope_group(groups[gi]));
             } else {

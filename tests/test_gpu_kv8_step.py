@@ -157,6 +157,14 @@ def test_many_rows():
     m.step(batch_of(m.cfg.vocab, 2, [EmbChunk(0, 300, 84, True, "mean")], [], [DecodeRow(3, 383)], a))
 
 
+@pytest.mark.parametrize("two", [False, True])
+def test_projection_in_two_parts(two):
+    """Wide enough that the projection of few rows is split over its sum: the append adds the parts."""
+    m = Served("bf16", two, two, cfg=tiny_config("bf16").replace(d_model=1024, n_q_heads=8, n_kv_heads=4, head_dim=128, d_ff=512))
+    a = m.step(batch_of(m.cfg.vocab, 1, [EmbChunk(0, 0, 50, True, "mean")], [GenChunk(3, 0, 40, True), GenChunk(5, 0, 3, True)]))
+    m.step(batch_of(m.cfg.vocab, 2, [], [], [DecodeRow(3, 40), DecodeRow(5, 3)], a))
+
+
 def drawn_steps(v):
     yield batch_of(v, 1, [EmbChunk(0, 0, 20, False, "mean")], [GenChunk(3, 0, 40, True), GenChunk(4, 0, 18, True)])
     for i in range(4):
