@@ -132,10 +132,11 @@ __global__ __launch_bounds__(NT) void append8_kernel(Append8 a) {
             const int tk = k / half, pr = k % half;
             // turns modulo one in double: far positions keep their angle
             const double c = (double)(block * kPage8 + first + tk) * turns[pr];
-            const float f = (float)(2.0 * (c - rint(c)));
+            const double r = 2.0 * (c - rint(c));
+            const float f = (float)r, rest = (float)(r - (double)f) * (float)M_PI;     // what fp32 leaves of the angle
             float sn, cs;
             sincospif(f, &sn, &cs);
-            turn[tk][pr] = float2{cs * a.magnitude, sn * a.magnitude};
+            turn[tk][pr] = float2{fmaf(-sn, rest, cs) * a.magnitude, fmaf(cs, rest, sn) * a.magnitude};
         }
     }
     __syncthreads();

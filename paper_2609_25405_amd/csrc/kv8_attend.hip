@@ -2,7 +2,7 @@
 //
 // Both kernels turn codes into bf16 by v_cvt_scalef32_pk_bf16_fp8 (two codes an instruction, exact) and
 // multiply on bf16 MFMA, with an online softmax in fp32 (exp2 domain).  fp32 rows go through the
-// same products in parts: q as three bf16 parts (exact), the weights as two (16 bits), each part a
+// same products in parts: q and the weights as three bf16 parts each (24 bits, all of an fp32 value), each part a
 // product of its own into the same sums.
 //
 // Small items ((rows, query heads of one KV head) pairs of a segment, at most 16): the pairs are the 16 columns
@@ -97,7 +97,7 @@ __device__ __forceinline__ float add_pair(uint32_t w, float c) {
 
 template <typename T> struct Rows8;
 template <> struct Rows8<bf16> { static constexpr int NQ = 1, NP = 1; };
-template <> struct Rows8<float> { static constexpr int NQ = 3, NP = 2; };
+template <> struct Rows8<float> { static constexpr int NQ = 3, NP = 3; };
 
 __device__ __forceinline__ void store4(float *p, float a, float b, float c, float d) { *(float4 *)p = float4{a, b, c, d}; }
 __device__ __forceinline__ void store4(bf16 *p, float a, float b, float c, float d) {

@@ -6,7 +6,7 @@ Bounds (a rounding is off by half a step: relative 2^-8 to bfloat16, 2^-24 to fp
     gain, sine and cosine (2 steps each), the rotation's three roundings: under 2^5 roundings of 2^-24;
   * held values: half a step of e4m3 under the page's own scale (2^-4 of the value, 2^-10 of the scale below
     2^-6), plus the same arithmetic; values that no arithmetic touches are the definition's bit for bit;
-  * attention: softmax weights off by 2^-8 (bfloat16 rows) or 2^-16 (fp32 rows, two parts), the output's own
+  * attention: softmax weights off by 2^-8 (bfloat16 rows) or less than 2^-16 (fp32 rows, three parts), the output's own
     rounding, and fp32 scores: products of at most 128 terms err by less than 2^-19 of the sum of their
     magnitudes, an absolute error of the exponent, so of every weight (twice: weight and sum); sums over keys
     add 2^-16 of the magnitudes.

@@ -79,6 +79,25 @@ def test_long_ranges_come_in_pieces(dtype):
     attend(b, segs)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [False, True])
+def test_tiles_of_many_pages(dtype, bad):
+    """So many rows that no range is cut: a tile walks over more pages than it keeps at a time, a bad one among
+    the later ones."""
+    shape = ops.HeadShape(64, 8, 128, dtype=dtype)
+    segs = [(0, 7411, 1030), (1, 4090, 20)]
+    b = Both(shape, 2, 528, seed=61)
+    b.fill({s: o + n for s, o, n in segs})
+    counts, items = ops.RaggedRows(shape, 1050, 2, 8441).items(b.kv, segs)
+    assert (items[counts[0]:, 6] - items[counts[0]:, 5]).max() > 8000
+    skip = ()
+    if bad:
+        b.table[0][300], b.table[1][256], skip = b.kv.n_pages, -3, (b.kv.n_pages, -3)
+        b.kv.set_block_table(b.table)
+        b.ref.val = [np.concatenate([v, np.zeros((4,) + v.shape[1:])]) for v in b.ref.val]
+    attend(b, segs, some={0, 1, 517, 1028, 1029, 1030, 1035, 1036, 1049}, skip=skip)
+
+
 def test_many_rows_with_uneven_contexts():
     shape = ops.HeadShape(8, 2, 128)
     rng = np.random.default_rng(4)
