@@ -454,25 +454,22 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
     const int32_t *table = a.p.table + (size_t)seq * a.p.max_blocks;
     const int nkb = (key1 - key0 + St::KEYS - 1) / St::KEYS, last = (key1 - 1) / kPage8;
 
-    const T *qp = (const T *)a.q + (size_t)(row0 + tok) * a.q_stride + (size_t)h * HD;
-    bf16x8 q[KS][R::NQ];
-#pragma unroll
-    for (int k = 0; k < KS; ++k) load_q<T, R::NQ>(qp + 16 * k + 8 * half, q[k]);
-
     int w0 = key0 / kPage8;            // first page of the window (a multiple of 4)
-    bool bad = false;
-    auto load_window = [&]() {
-        const int p = w0 + tid;
-        if (p > last) return;
-        const int id = table[p];
+    auto window_id = [&]() { return table[min(w0 + tid, last)]; };        // (places past the last page repeat it)
+    auto load_window = [&](int id) {
         const bool ok = id >= 0 && id < a.p.n_pages;
         const size_t head = (size_t)(ok ? id : 0) * a.p.nkv + g;
         win_page[tid] = ok ? id : -1;
         win_scale[tid] = ok ? float2{a.p.ks[head], a.p.vs[head]} : float2{1.f, 1.f};
         if (!ok) flag_error(a.p.err, ORTHRUS_DEVERR_PAGE);
-        bad |= !ok;
     };
     static_assert(kWindow == 256, "a page a thread");
+    auto window_bad = [&]() {
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < kWindow; i += 64) bad |= win_page[i + lane] < 0;
+        return __ballot(bad) != 0;
+    };
 
     // Wave w takes page w of each block: lane (key, part) reads KL x 16 dims of a key, lane (dim % 16, quad) KL x 16
     // bytes of the page's values.
@@ -520,25 +517,25 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
     float k_mul, v_mul;
     const int k_dst = krow * St::KRB + St::kchunk(krow, kpart * (KL * 2)) * 16;      // chunk i enters by exclusive or
     const int v_dst = St::KBYTES + wave * St::VPAGE + vlane * 32 + St::vchunk(vlane, vquad / 2) * 16 + (vquad % 2) * 8;
-    auto put_k = [&](int buf, int i) {
-        const uint2 lo = word_bf16(kr[i / 2][2 * (i % 2)], k_mul), hi = word_bf16(kr[i / 2][2 * (i % 2) + 1], k_mul);
+    auto put_k = [&](int buf, int i, const u32x4 (&r)[KL]) {
+        const uint2 lo = word_bf16(r[i / 2][2 * (i % 2)], k_mul), hi = word_bf16(r[i / 2][2 * (i % 2) + 1], k_mul);
         *(u32x4 *)(smem + buf * St::BYTES + (k_dst ^ (i * 16))) = u32x4{lo.x, lo.y, hi.x, hi.y};
     };
-    auto put_v = [&](int buf, int i) {
-        *(uint2 *)(smem + buf * St::BYTES + i * 512 + v_dst) = word_bf16(vr[i / 4][i % 4], v_mul);       // dim 16 i + vlane
+    auto put_v = [&](int buf, int i, const u32x4 (&r)[KL]) {
+        *(uint2 *)(smem + buf * St::BYTES + i * 512 + v_dst) = word_bf16(r[i / 4][i % 4], v_mul);       // dim 16 i + vlane
     };
-    auto keep_k = [&]() {
-        if (kvalid == 0) {         // (wave-uniform, as the next)
+    auto keep_k = [&](int valid, u32x4 (&r)[KL]) {
+        if (valid == 0) {          // (wave-uniform, as the next)
 #pragma unroll
-            for (int j = 0; j < KL; ++j) kr[j] = u32x4{0u, 0u, 0u, 0u};
+            for (int j = 0; j < KL; ++j) r[j] = u32x4{0u, 0u, 0u, 0u};
         }
     };
-    auto keep_v = [&]() {
-        if (vvalid < kPage8) {
-            const int n = max(0, min(4, vvalid - 4 * vquad));
+    auto keep_v = [&](int valid, u32x4 (&r)[KL]) {
+        if (valid < kPage8) {
+            const int n = max(0, min(4, valid - 4 * vquad));
             const uint32_t keep = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1;
 #pragma unroll
-            for (int j = 0; j < KL; ++j) vr[j] &= keep;
+            for (int j = 0; j < KL; ++j) r[j] &= keep;
         }
     };
     auto scales = [&]() {
@@ -601,8 +598,43 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
         return (uint32_t)__builtin_amdgcn_readfirstlane(bad);
     };
 
-    load_window();
-    bool any_bad = __syncthreads_or(bad);      // then each block's pages are looked at again
+    // The codes of the first keys and values start before their scales are known (their pages straight from the table), the
+    // query rows behind them: everything is on its way after one read of the table.  (One by one as in the loop the first
+    // scores were there 5 us after the start, now after 3.5; 4 fresh prompts of 400 to 623 tokens 26.5 -> 24.9 us.)
+    const int ids = window_id();
+    auto first_page = [&](int b) {
+        const int id = table[min(key0 / kPage8 + 4 * b + wave, last)];
+        return id >= 0 && id < a.p.n_pages ? id : -1;
+    };
+    const int first_pages[3] = {first_page(0), first_page(1), first_page(2)};
+    u32x4 k0[KL], k1[KL], v0[KL];
+    int k_valid[2], v_valid;
+    auto keep = [&](u32x4 (&to)[KL], const u32x4 (&from)[KL]) {
+#pragma unroll
+        for (int j = 0; j < KL; ++j) to[j] = from[j];
+    };
+    page = vpage = first_pages[0];
+    fetch_k(0);
+    keep(k0, kr);
+    k_valid[0] = kvalid;
+    fetch_v(0);
+    keep(v0, vr);
+    v_valid = vvalid;
+    page = vpage = first_pages[1];
+    fetch_k(1);
+    keep(k1, kr);
+    k_valid[1] = kvalid;
+    fetch_v(1);
+    page = first_pages[2];
+    fetch_k(2);
+    __builtin_amdgcn_sched_barrier(0);
+    load_window(ids);
+    const T *qp = (const T *)a.q + (size_t)(row0 + tok) * a.q_stride + (size_t)h * HD;
+    bf16x8 q[KS][R::NQ];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) load_q<T, R::NQ>(qp + 16 * k + 8 * half, q[k]);
+    lds_barrier();
+    bool any_bad = window_bad();               // then each block's pages are looked at again
 
     // Block b's weights run beside block b + 1's scores, and its products beside the next codes' way into LDS (keys one
     // block ahead of values): the compiler keeps no such order by itself, so every product is a slot with its share of the
@@ -617,8 +649,8 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
         for (int i = 0; i < AHEAD; ++i) ring[i] = k_frag(P ^ 1, i);
         raise(b, any_bad ? bad_pages(b) : 0, s, mx);
         // (no branch between the slots: the compiler would move their work past it)
-        keep_v();
-        keep_k();
+        keep_v(vvalid, vr);
+        keep_k(kvalid, kr);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -656,8 +688,8 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
             for (int n = 0; n < R::NP; ++n) acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(NA + i) % AHEAD], pf[i / DB][n], acc[i % DB], 0, 0, 0);
             if (i + AHEAD < NB) ring[(NA + i) % AHEAD] = v_frag(P, i + AHEAD);
             // into the buffers that iteration b - 1 read; the registers take the next ones, most of a step ahead
-            if (i < NB / 2) put_v(P ^ 1, i);
-            else if (i % 2 == 1) put_k(P, (i - NB / 2) / 2);
+            if (i < NB / 2) put_v(P ^ 1, i, vr);
+            else if (i % 2 == 1) put_k(P, (i - NB / 2) / 2, kr);
             if (i == NB / 4) look_up(b + 3);
             if (i == NB / 2) fetch_v(b + 2);
             if (i == NB - 2) use_page();
@@ -669,36 +701,32 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
         if (4 * (b + 4) + key0 / kPage8 - w0 >= kWindow && w0 + kWindow <= last) {
             lds_barrier();             // everyone has looked up block b + 3
             w0 += kWindow;
-            load_window();
-            any_bad |= (bool)__syncthreads_or(bad);
+            load_window(window_id());
+            lds_barrier();
+            any_bad |= window_bad();
         }
         lds_barrier();
     };
+    keep_k(k_valid[0], k0);
+    keep_v(v_valid, v0);
     look_up(0);
     use_page();
-    fetch_k(0);
     next_v();
-    fetch_v(0);
-    keep_k();
-    keep_v();
     scales();
 #pragma unroll
-    for (int i = 0; i < 2 * KL; ++i) put_k(0, i);
+    for (int i = 0; i < 2 * KL; ++i) put_k(0, i, k0);
 #pragma unroll
-    for (int i = 0; i < 4 * KL; ++i) put_v(0, i);
+    for (int i = 0; i < 4 * KL; ++i) put_v(0, i, v0);
+    keep_k(k_valid[1], k1);
     look_up(1);
     use_page();
-    fetch_k(1);
     next_v();
-    fetch_v(1);
-    keep_k();
     scales();
 #pragma unroll
-    for (int i = 0; i < 2 * KL; ++i) put_k(1, i);
+    for (int i = 0; i < 2 * KL; ++i) put_k(1, i, k1);
     look_up(2);
     use_page();
-    fetch_k(2);
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -709,7 +737,7 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
         for (int n = 0; n < R::NQ; ++n) sa[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(0, i), q[i / 2][n], sa[i % 2], 0, 0, 0);
 #pragma unroll
     for (int e = 0; e < 32; ++e) mx = fmaxf(mx, sa[e / 16][e % 16]);
-    __syncthreads();
+    lds_barrier();
     for (int b = 0; b < nkb; b += 2) {
         step(b, std::integral_constant<int, 0>{}, sa, sb);
         if (b + 1 < nkb) step(b + 1, std::integral_constant<int, 1>{}, sb, sa);
