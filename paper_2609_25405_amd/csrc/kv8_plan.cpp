@@ -23,6 +23,9 @@ constexpr int kSlotsSmall = 768, kMinPieceSmall = 1024;
 // Few of them run with eight waves each, cut for fewer workgroups (one row of 4000 keys over 8 KV heads 12.5 us in
 // pieces of at least 512 keys, 14.5 of 1024; 16 rows of 2000 17.6 us in 192 slots, 18.8 in 256, 21.9 in 384).
 constexpr int kWideItems = 256, kSlotsWide = 192, kMinPieceWide = 512;
+// ... but not at all where none has more than two steps a wave (one row of 1000 keys 9.5 us whole, 11.0 in two pieces; of 1300 12.3
+// and 10.2; 4 rows of 1400 13.6 and 11.6).
+constexpr int kMostWhole = 1024;
 // Tiles run two workgroups a CU; items i and kCus + i of a launch share one, so the second round comes shortest first
 // (4 fresh prompts of 400 to 623 tokens 26.9 -> 26.5 us).
 constexpr int kCus = 256, kSlotsTile = 2 * kCus, kMinPieceTile = 1024;
@@ -117,10 +120,11 @@ int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, co
     std::vector<std::array<int32_t, kMerge8Ints>> merges;
     using Item = std::array<int32_t, kItem8Ints>;
     // longest first, so that the launch does not end on a long item; equal ones in the rows' order
-    auto cut = [&](std::vector<Range> &ranges, int64_t piece, int most_pieces, int slots_each) {
+    auto cut = [&](std::vector<Range> &ranges, int64_t piece, int64_t whole, int most_pieces, int slots_each) {
         std::vector<std::pair<int64_t, Item>> items;
         int pieces = 0;
         std::stable_sort(ranges.begin(), ranges.end(), [](const Range &a, const Range &b) { return a.work > b.work; });
+        if (!ranges.empty() && ranges[0].work <= whole) piece = whole;       // none is worth a merge
         for (const Range &r : ranges) {
             // (the nearest count: one piece too many for some ranges would be a second round of the launch)
             int m = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxPieces, (r.work + piece / 2) / piece));
@@ -145,8 +149,9 @@ int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, co
     };
     p.joint = !small.empty() && !tiles.empty();
     p.wide = !p.joint && (int)small.size() <= kWideItems;
-    const auto is = cut(small, p.wide ? piece_keys(keys_small, kSlotsWide, kMinPieceWide) : piece_keys(keys_small, kSlotsSmall, kMinPieceSmall), kMaxSmallPieces, 1);
-    auto it = cut(tiles, piece_keys(keys_tiles, kSlotsTile, kMinPieceTile), kMaxTilePieces, kTileRows8 / kSmallCols);
+    const auto is = p.wide ? cut(small, piece_keys(keys_small, kSlotsWide, kMinPieceWide), kMostWhole, kMaxSmallPieces, 1)
+                           : cut(small, piece_keys(keys_small, kSlotsSmall, kMinPieceSmall), 0, kMaxSmallPieces, 1);
+    auto it = cut(tiles, piece_keys(keys_tiles, kSlotsTile, kMinPieceTile), 0, kMaxTilePieces, kTileRows8 / kSmallCols);
     if (it.size() > (size_t)kCus) std::reverse(it.begin() + kCus, it.begin() + std::min<size_t>(it.size(), 2 * kCus));
     p.n_small = (int)is.size();
     p.n_tiles = (int)it.size();
