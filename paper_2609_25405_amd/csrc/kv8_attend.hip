@@ -159,6 +159,18 @@ template <typename T, int HD> __global__ __launch_bounds__(256) void attend8_mer
     const int cols = min(kSmallCols, me[M8_LEN] * a.p.group - c0);
     if (cols <= 0) return;
     const int slot0 = me[M8_SLOT] + (int)blockIdx.y;
+    // the first pieces' sums are on their way while the factors are taken
+    constexpr int UNITS = kSmallCols * HD / 4 / 256, FIRST = 4;
+    const size_t step = (size_t)slots * 16 * (HD + kPartialPad);
+    auto sums_of = [&](int u) { return partial_of<HD>(a, slot0, u / (HD / 4)) + kPartialPad + u % (HD / 4) * 4; };
+    f32x4 early[UNITS][FIRST];
+#pragma unroll
+    for (int k = 0; k < UNITS; ++k) {
+        const float *p = sums_of(min(tid + 256 * k, cols * (HD / 4) - 1));
+#pragma unroll
+        for (int i = 0; i < FIRST; ++i)
+            if (i < n) early[k][i] = *(const f32x4 *)(p + i * step);
+    }
     {
         const int col = tid / TPC;
         float M = -INFINITY, L = 0.f;
@@ -181,13 +193,17 @@ template <typename T, int HD> __global__ __launch_bounds__(256) void attend8_mer
         if (tid % TPC == 0) inv[col] = L != 0.f ? 1.f / L : 0.f;
     }
     __syncthreads();
-    const size_t step = (size_t)slots * 16 * (HD + kPartialPad);
-    for (int u = tid; u < cols * (HD / 4); u += 256) {
-        const int col = u / (HD / 4), d = u % (HD / 4) * 4;
+#pragma unroll
+    for (int k = 0; k < UNITS; ++k) {
+        const int u = tid + 256 * k, col = u / (HD / 4), d = u % (HD / 4) * 4;
+        if (col >= cols) break;
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        const float *p = partial_of<HD>(a, slot0, col) + kPartialPad + d;
+#pragma unroll
+        for (int i = 0; i < FIRST; ++i)
+            if (i < n) sum += early[k][i] * f[col][i];
+        const float *p = sums_of(u);
 #pragma unroll 8
-        for (int i = 0; i < n; ++i) sum += *(const f32x4 *)(p + i * step) * f[col][i];
+        for (int i = FIRST; i < n; ++i) sum += *(const f32x4 *)(p + i * step) * f[col][i];
         const int c = c0 + col, row = me[M8_ROW] + c / a.p.group, h = me[M8_HEAD] * a.p.group + c % a.p.group;
         store4((T *)a.out + (size_t)row * a.out_stride + (size_t)h * HD + d, sum[0] * inv[col], sum[1] * inv[col], sum[2] * inv[col],
                sum[3] * inv[col]);
