@@ -5,7 +5,8 @@ and a greedy sampler.
 
 The compute lives in liborthrus.so (hand-written HIP kernels behind the C ABI declared in
 include/orthrus.h).  ``_abi`` mirrors that ABI with the same names; ``runtime`` holds device
-memory in torch tensors and marshals arguments.  Build with
+memory in torch tensors and marshals arguments; ``ops`` does so for the 8-bit cache and token
+scores of include/orthrus/.  Build with
 ``python -m paper_2609_25405_amd.build``.
 """
 from ._abi import (LIB_PATH, OrthrusError, load, orthrus_device_error, orthrus_model_create,

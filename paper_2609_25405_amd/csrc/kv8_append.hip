@@ -9,6 +9,10 @@
 // A head row of HD dims lies over HD / 16 lanes; lane i holds dims 8 i .. 8 i + 7 and HD / 2 + 8 i ..
 // + 7, two 16-byte loads of bf16, so that the pairs (i, i + HD / 2) of a head that turns whole, and
 // the pairs (2 i, 2 i + 1), are in one lane; pairs of a head that turns in part meet through LDS.
+//
+// Bound by the rows' bytes: 8.8 k bf16 rows of 32 + 2 x 8 heads of 128 dims in 47 us, 4.2 TB/s of 110 MB read and 90
+// written; 256 decode rows with norms in 7.6 us, one round of waves that wait for two dependent reads.  The read-back of the
+// same rows takes 14.7 and 5.6 us (18 MB in, 36 out).
 #include <type_traits>
 
 #include "kv8.hpp"
