@@ -74,8 +74,9 @@ size_t orthrus_rows_workspace_bytes(const orthrus_rows *r, int32_t max_rows, int
 
 /* Plans the rows of the following calls: segment i's rows follow segment i - 1's.  Validates before
  * anything is enqueued: EDESC (seq outside [0, n_seq), offset < 0, len < 1), EDUPSEQ (a sequence in
- * two segments), ECAPACITY (past the block table, or workspace too small), EUNSUPPORTED (stream
- * under capture).  Uploads the plan into `workspace` (256-byte aligned, cleared once by
+ * two segments), ECAPACITY (past the block table, more than 2^23 rows times KV heads, or workspace too small),
+ * EUNSUPPORTED (stream under capture).  Sequences may share pages that are only read; the pages that one segment
+ * appends to are no other segment's.  Uploads the plan into `workspace` (256-byte aligned, cleared once by
  * orthrus_workspace_init) on `stream`; n = 0 is a plan without rows.
  * The plan holds until the next one of this handle, for any layer of any cache that has its
  * sequences.  The handle belongs to the device that is current at its first plan (EINVAL on another).
@@ -115,7 +116,7 @@ int orthrus_kv8_read(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer
  * negative or not finite).  q, out: device [rows][stride] of the shape's dtype, n_q head_dim values a
  * row; strides multiples of 8 elements, bases 16-byte aligned (EINVAL).  Scores, softmax and sums in
  * fp32; bfloat16 rows round the softmax weights to bfloat16 before the product with the values, fp32 rows keep
- * 16 bits of them.  Keys of a page outside [0, n_pages) are skipped (ORTHRUS_DEVERR_PAGE); a row
+ * them whole.  Keys of a page outside [0, n_pages) are skipped (ORTHRUS_DEVERR_PAGE); a row
  * left without keys is zero. */
 int orthrus_kv8_attend(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer, const void *q, int64_t q_stride,
                        float scale, void *out, int64_t out_stride, void *stream);

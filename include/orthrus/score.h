@@ -30,7 +30,8 @@ size_t orthrus_logprobs_bytes(int32_t rows, int32_t vocab, int32_t n_top);
  * top_logprobs are NaN, its rank and top_ids as ordered.  Sums are taken in fp32 in a fixed order.
  * workspace: device, orthrus_logprobs_bytes(), 16-byte aligned, one call in flight; may be NULL if that is 0.
  * EINVAL: negative sizes, vocab < 1, n_top outside [0, min(vocab, ORTHRUS_MAX_TOP)], row_stride < vocab, a null
- * pointer that is needed; ECAPACITY: ws_bytes too small.  rows = 0 is a no-op. */
+ * pointer that is needed; ECAPACITY: ws_bytes too small, 2^22 or more rows (or rows times slices of 32 k entries)
+ * or more than 2^30 entries a row.  rows = 0 is a no-op. */
 int orthrus_logprobs(const float *logits, int64_t row_stride, int32_t rows, int32_t vocab, const int32_t *tokens,
                      int32_t n_top, float *logprob, float *entropy, int32_t *rank, int32_t *top_ids, float *top_logprobs,
                      void *workspace, size_t ws_bytes, void *stream);

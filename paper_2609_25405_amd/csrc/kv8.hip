@@ -42,7 +42,10 @@ namespace {
 
 #define HIP_TRY(expr)                                   \
     do {                                                \
-        if ((expr) != hipSuccess) return ORTHRUS_EHIP;  \
+        if ((expr) != hipSuccess) {                     \
+            (void)hipGetLastError();                    \
+            return ORTHRUS_EHIP;                        \
+        }                                               \
     } while (0)
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }

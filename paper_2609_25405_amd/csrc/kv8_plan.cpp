@@ -87,8 +87,8 @@ int plan_rows8(const orthrus_head_shape &s, const std::vector<double> &turns, co
         p.need_seq = std::max(p.need_seq, g.seq + 1);
         p.need_blocks = std::max(p.need_blocks, (int)((end + kPage8 - 1) / kPage8));
     }
-    // work lists are indexed in 32 bits
-    if (T > (1LL << 24) || T * nkv > (1LL << 26)) return ORTHRUS_ECAPACITY;
+    // a launch has fewer than 2^32 threads, up to 256 for each row and KV head
+    if (T * nkv > (1LL << 23)) return ORTHRUS_ECAPACITY;
     p.T = (int)T;
 
     std::vector<int32_t> units;

@@ -463,7 +463,9 @@ int orthrus_logprobs(const float *logits, int64_t row_stride, int32_t rows, int3
     if (rows < 0 || vocab < 1 || n_top < 0 || n_top > std::min(vocab, ORTHRUS_MAX_TOP) || row_stride < vocab) return ORTHRUS_EINVAL;
     if (rows == 0) return ORTHRUS_OK;
     if (!logits || ((logprob || rank) && !tokens) || (n_top == 0 && (top_ids || top_logprobs))) return ORTHRUS_EINVAL;
-    if (vocab > (1 << 30) || (int64_t)rows * score_slices(vocab) > INT32_MAX) return ORTHRUS_ECAPACITY;
+    if ((uintptr_t)logits & 3) return ORTHRUS_EINVAL;
+    // a launch has fewer than 2^32 threads, up to 1024 for each slice
+    if (vocab > (1 << 30) || (int64_t)rows * score_slices(vocab) >= (1 << 22)) return ORTHRUS_ECAPACITY;
     const size_t need = score_bytes(rows, vocab, n_top);
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 15))) return ORTHRUS_EINVAL;
     if (ws_bytes < need) return ORTHRUS_ECAPACITY;

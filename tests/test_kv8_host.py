@@ -249,6 +249,24 @@ def test_scores_definition():
     assert math.isclose(ent, -sum(v * math.log(v) for v in p if v > 0)) and np.allclose(tops, np.log(p[[1, 3, 0]]))
 
 
+def test_work_beyond_one_launch_is_refused():
+    """A launch has fewer than 2^32 threads: more rows times heads, or rows of logits, than it can serve."""
+    shape = ops.HeadShape(8, 8, 64)
+    kv = ops.DeviceKV8(shape, 1, 1, 1, 65537, device="cpu")
+    rows = ops.RaggedRows(shape, 1, 1, 1, device="cpu")
+    counts, _ = rows.items(kv, [(0, 0, 2 ** 20)])
+    assert counts[1] == 8 * 2 ** 20 // 128 + counts[3] // 8 - counts[2]
+    with code_of(A.ORTHRUS_ECAPACITY):
+        rows.items(kv, [(0, 0, 2 ** 20 + 1)])
+    x = torch.zeros(8)
+    at = -(-x.data_ptr() // 16) * 16
+
+    def call(p, n, vocab=1):
+        return O.load().orthrus_logprobs(p, vocab, n, vocab, None, 0, None, None, None, None, None, None, 0, None)
+    assert call(at, 2 ** 22) == call(at, 2 ** 31 - 1) == call(at, 2 ** 21, 60000) == A.ORTHRUS_ECAPACITY
+    assert call(at + 2, 1) == A.ORTHRUS_EINVAL
+
+
 def test_step_refusals():
     """orthrus_step_kv8 turns away what it cannot run before it touches a device."""
     from paper_2609_25405_amd import runtime as R
