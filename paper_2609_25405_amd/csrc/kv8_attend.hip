@@ -106,6 +106,20 @@ __device__ __forceinline__ void store4(bf16 *p, float a, float b, float c, float
     *(uint2 *)p = uint2{pack_bf16x2(a, b), pack_bf16x2(c, d)};
 }
 
+// A pair whose every score is minus infinity has no weights: its output is not a number, unlike that of a pair
+// without keys.  Its sum of weights, which would be zero, is marked.
+constexpr float kNoWeights = -1.f;
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : l < 0.f ? NAN : 1.f / l; }
+// whether row `row` of the item at `at` of the plan has a key in the item's range (both read again: this is rare, registers are not)
+__device__ __forceinline__ bool has_key(const Attend8 &a, int at, int row) {
+    const int32_t *it = a.p.meta + at, *table = a.p.table + (size_t)it[A8_SEQ] * a.p.max_blocks;
+    for (int k = it[A8_KEY0]; k < min(it[A8_KEY1], it[A8_POS] + row + 1); k += kPage8) {
+        const int id = table[k / kPage8];
+        if (id >= 0 && id < a.p.n_pages) return true;
+    }
+    return false;
+}
+
 // One (row, query head) pair, by one wave, key after key, so that nothing the row does not see enters its
 // sums: for pairs whose sums met something not finite in a masked place (zero times it is not zero).
 // Lane l holds dims l (and l + 64).
@@ -116,6 +130,7 @@ __device__ void pair_key_by_key(const Attend8 &a, int seq, int head, int pos, in
     const int lane = threadIdx.x & 63;
     const int32_t *table = a.p.table + (size_t)seq * a.p.max_blocks;
     float q[N], m = -INFINITY, l = 0.f;
+    bool any = false;
 #pragma unroll
     for (int d = 0; d < N; ++d) {
         q[d] = to_f32(qp[lane + 64 * d]);
@@ -124,6 +139,7 @@ __device__ void pair_key_by_key(const Attend8 &a, int seq, int head, int pos, in
     for (int key = key0; key < min(key1, pos + 1); ++key) {
         const int page = table[key / kPage8], slot = key % kPage8;
         if (page < 0 || page >= a.p.n_pages) continue;
+        any = true;
         const size_t at = (size_t)page * a.p.nkv + head;
         const uint8_t *kp = a.p.k + at * (kPage8 * HD) + slot * HD, *vp = a.p.v + at * (kPage8 * HD) + (slot / 4) * (4 * HD) + slot % 4;
         float s = 0.f;
@@ -142,7 +158,7 @@ __device__ void pair_key_by_key(const Attend8 &a, int seq, int head, int pos, in
         m = mn;
     }
     m_out = m;
-    l_out = l;
+    l_out = l == 0.f && any ? kNoWeights : l;
 }
 
 // ------------------------------------------------------------------ pieces of a key range
@@ -175,7 +191,7 @@ template <typename T, int HD> __global__ __launch_bounds__(256) void attend8_mer
     }
     {
         const int col = tid / TPC;
-        float M = -INFINITY, L = 0.f;
+        float M = -INFINITY, L = 0.f, least = 0.f;
         if (col < cols) {
             for (int i = tid % TPC; i < n; i += TPC) M = fmaxf(M, partial_of<HD>(a, slot0 + i * slots, col)[0]);
         }
@@ -185,14 +201,18 @@ template <typename T, int HD> __global__ __launch_bounds__(256) void attend8_mer
             for (int i = tid % TPC; i < n; i += TPC) {
                 const float *p = partial_of<HD>(a, slot0 + i * slots, col);
                 // (a piece whose every score was not a number has a sum but no maximum)
-                const float w = p[0] == -INFINITY ? (p[1] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(p[0] - M);
+                const float w = p[0] == -INFINITY ? (p[1] == 0.f || p[1] == kNoWeights ? 0.f : 1.f) : __builtin_amdgcn_exp2f(p[0] - M);
                 f[col][i] = w;
+                least = fminf(least, p[1]);
                 L = fmaf(p[1], w, L);
             }
         }
 #pragma unroll
-        for (int o = 1; o < TPC; o *= 2) L += __shfl_xor(L, o, 64);
-        if (tid % TPC == 0) inv[col] = L != 0.f ? 1.f / L : 0.f;
+        for (int o = 1; o < TPC; o *= 2) {
+            L += __shfl_xor(L, o, 64);
+            least = fminf(least, __shfl_xor(least, o, 64));
+        }
+        if (tid % TPC == 0) inv[col] = inverse(L == 0.f ? least : L);
     }
     __syncthreads();
 #pragma unroll
@@ -382,6 +402,8 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
         for (int d = 0; d < DB; ++d) *(f32x4 *)(sums(wave, c) + 16 * d + 4 * qd) = acc[d];
     }
     __syncthreads();
+    int group = a.p.group;
+    asm("" : "+v"(group));       // its reciprocal is taken anew: kept through the loop it would cost a spill
     // merge the waves in order; four dims a thread
     for (int o = tid; o < cols * (HD / 4); o += 64 * NW) {
         const int col = o / (HD / 4), d = o % (HD / 4) * 4;
@@ -396,6 +418,7 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
             L += lw * f;
             sum += *(const f32x4 *)(sums(w, col) + d) * f;
         }
+        if (L == 0.f && has_key(a, a.off_small + kItem8Ints * index, col / group)) L = kNoWeights;
         if (slot >= 0) {
             float *pp = partial_of<HD>(a, slot, col);
             if (d == 0) {
@@ -404,8 +427,8 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
             }
             *(f32x4 *)(pp + kPartialPad + d) = sum;
         } else {
-            const float inv = L != 0.f ? 1.f / L : 0.f;
-            T *dst = (T *)a.out + (size_t)(row0 + col / a.p.group) * a.out_stride + (size_t)(g * a.p.group + col % a.p.group) * HD + d;
+            const float inv = inverse(L);
+            T *dst = (T *)a.out + (size_t)(row0 + col / group) * a.out_stride + (size_t)(g * group + col % group) * HD + d;
             store4(dst, sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv);
         }
     }
@@ -418,7 +441,7 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
             for (int w = 0; w < NW; ++w)
                 for (int d = lane; d < HD; d += 64) bad |= !(fabsf(sums(w, col)[d]) < INFINITY);
             if (__ballot(bad) == 0) continue;
-            const int t = col / a.p.group, hh = g * a.p.group + col % a.p.group;
+            const int t = col / group, hh = g * group + col % group;
             if (pos0 + t + 1 >= key1) continue;        // nothing masked
             float o[HD / 64], mm, ll;
             pair_key_by_key<T, HD>(a, seq, g, pos0 + t, key0, key1, (const T *)a.q + (size_t)(row0 + t) * a.q_stride + (size_t)hh * HD, mm, ll, o);
@@ -430,7 +453,7 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
 #pragma unroll
             for (int d = 0; d < HD / 64; ++d) {
                 if (slot >= 0) pp[kPartialPad + lane + 64 * d] = o[d];
-                else ((T *)a.out)[(size_t)(row0 + t) * a.out_stride + (size_t)hh * HD + lane + 64 * d] = from_f32<T>(ll != 0.f ? o[d] / ll : 0.f);
+                else ((T *)a.out)[(size_t)(row0 + t) * a.out_stride + (size_t)hh * HD + lane + 64 * d] = from_f32<T>(o[d] * inverse(ll));
             }
         }
     }
@@ -763,6 +786,7 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
     {
         const float2 p = partner32(l);
         l = p.x + p.y;
+        if (l == 0.f && has_key(a, a.off_tiles + kItem8Ints * index, tok)) l = kNoWeights;
     }
     // sums that are not finite: from what the pair sees, or from zero weights times something that is not finite
     // in a masked place; told apart key by key
@@ -786,7 +810,7 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
 #pragma unroll
         for (int d = 0; d < HD / 64; ++d) {
             if (slot >= 0) pp[kPartialPad + lane + 64 * d] = o[d];
-            else ((T *)a.out)[(size_t)(row0 + t) * a.out_stride + (size_t)hh * HD + lane + 64 * d] = from_f32<T>(ll != 0.f ? o[d] / ll : 0.f);
+            else ((T *)a.out)[(size_t)(row0 + t) * a.out_stride + (size_t)hh * HD + lane + 64 * d] = from_f32<T>(o[d] * inverse(ll));
         }
     }
     if (c < cols && !(odd_cols >> col & 1)) {
@@ -803,7 +827,7 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
                     *(f32x4 *)(pp + kPartialPad + d * 32 + k * 8 + half * 4) =
                         f32x4{acc[d][4 * k], acc[d][4 * k + 1], acc[d][4 * k + 2], acc[d][4 * k + 3]};
         } else {
-            const float inv = l != 0.f ? 1.f / l : 0.f;
+            const float inv = inverse(l);
             T *dst = (T *)a.out + (size_t)(row0 + tok) * a.out_stride + (size_t)h * HD;
 #pragma unroll
             for (int d = 0; d < DB; ++d)

@@ -166,6 +166,37 @@ def test_odd_values_reach_only_the_rows_that_see_them(dtype, seg):
     assert rows.device_error() == 0
 
 
+@pytest.mark.parametrize("seg", [(0, 300, 1), (0, 9000, 1), (0, 50, 4), (0, 9000, 3), (0, 40, 90), (0, 9000, 40)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_row_of_scores_that_are_all_minus_infinity_is_not_a_number(seg, dtype):
+    """No weights can be taken of such scores, in one piece or several; a row without keys is zero beside it.  Rows of
+    other heads are as without it, and so is a row for which some keys only have such scores."""
+    shape = ops.HeadShape(4, 2, 64, dtype=dtype)
+    _, off, n = seg
+    b = Both(shape, 2, 600, seed=36)
+    b.fill({0: off + n, 1: 30})
+    k = b.kv.k.view(torch.uint8)
+    k[..., 5] = 0xb8                                                    # dim 5 of every key: -1 times the scale
+    b.kv.k_scale.copy_(torch.where(b.kv.k_scale > 0, 2.0 ** 5, b.kv.k_scale))
+    b.table[1][0] = -1
+    b.kv.set_block_table(b.table)
+    segs = [seg, (1, 9, 1)]
+    q = tensor(b.rng.normal(size=(n + 1, 256)), dtype)
+    rows, out, bad = b.rows(segs), *(torch.full((n + 1, 256), 5.0, device="cuda", dtype=shape.torch_dtype) for _ in range(2))
+    ops.kv8_attend(rows, b.kv, 0, q, out)
+    # a finite query whose scores overflow: -2^127 * 2^5 / sqrt(64)
+    q2 = q.clone()
+    q2.view(n + 1, 4, 64)[:n, 1] = 0
+    q2.view(n + 1, 4, 64)[:n, 1, 5] = 2.0 ** 127
+    ops.kv8_attend(rows, b.kv, 0, q2, bad)
+    torch.cuda.synchronize()
+    assert rows.device_error() == A.ORTHRUS_DEVERR_PAGE
+    o, w = out.view(n + 1, 4, 64), bad.view(n + 1, 4, 64)
+    assert w[:n, 1].isnan().all() and (w[n] == 0).all() and (o[n] == 0).all()
+    for h in (0, 2, 3):
+        assert torch.equal(o[:n, h], w[:n, h]) and o[:n, h].isfinite().all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_appended_tokens_are_seen_and_chunking_does_not_matter(dtype):
     """A prompt appended and attended at once, in chunks, and token by token."""
