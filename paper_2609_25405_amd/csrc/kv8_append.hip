@@ -11,7 +11,7 @@
 // the pairs (2 i, 2 i + 1), are in one lane; pairs of a head that turns in part meet through LDS.
 //
 // Bound by the rows' bytes: 8.8 k bf16 rows of 32 + 2 x 8 heads of 128 dims in 47 us, 4.2 TB/s of 110 MB read and 90
-// written; 256 decode rows with norms in 7.6 us, one round of waves that wait for two dependent reads.  The read-back of the
+// written; 256 decode rows with norms in 7.0 us, one round of waves that wait for two dependent reads.  The read-back of the
 // same rows takes 14.7 and 5.6 us (18 MB in, 36 out).
 #include <type_traits>
 
@@ -128,6 +128,28 @@ __global__ __launch_bounds__(NT) void append8_kernel(Append8 a) {
     const int rows = n * a.p.group;
     float xq[2][8];
     if (grp < rows) load_row(grp / a.p.group, g * a.p.group + grp % a.p.group, xq);
+    // and what a page that was begun before holds: its scales, and the values' words that new ones go into.  The values'
+    // tile is served by fours of slots, a wave one (or, one wave of few tokens, the two that these can touch).
+    constexpr int W = HD / 64, QUADS = NT == 64 ? 2 : 1;       // words a lane
+    const size_t head = (size_t)(ok ? page : 0) * a.p.nkv + g;
+    uint8_t *kp = a.p.k + head * (kPage8 * HD), *vp = a.p.v + head * (kPage8 * HD);
+    const int lane = tid % 64, wave = tid / 64;
+    auto quad_of = [&](int k) { return NT == 64 ? first / 4 + k : wave; };
+    auto words_of = [&](int q) { return (uint32_t *)(vp + q * (4 * HD)) + W * lane; };
+    float was[2] = {0.f, 0.f};
+    uint32_t old[QUADS][W] = {};
+    if (first > 0) {
+        was[0] = a.p.ks[head];
+        was[1] = a.p.vs[head];
+    }
+#pragma unroll
+    for (int k = 0; k < QUADS; ++k) {
+        const int q = quad_of(k), lo = first - 4 * q, hi = first + n - 4 * q;      // new slots of the four, before clamping
+        if (q < 4 && lo < 4 && hi > 0 && (lo > 0 || hi < 4)) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) old[k][j] = words_of(q)[j];
+        }
+    }
 
     const int half = a.rot / 2;
     if (half > 0) {
@@ -228,19 +250,14 @@ __global__ __launch_bounds__(NT) void append8_kernel(Append8 a) {
         if (i == 0) amax[which][t] = m;
     }
     __syncthreads();
-    const size_t head = (size_t)(ok ? page : 0) * a.p.nkv + g;
-    uint8_t *kp = a.p.k + head * (kPage8 * HD), *vp = a.p.v + head * (kPage8 * HD);
-    float scale[2], was[2];
+    float scale[2];
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
         float m = 0.f;
         for (int s = 0; s < n; ++s) m = fmaxf(m, amax[w][s]);
         scale[w] = scale_of(m);
-        was[w] = scale[w];
-        if (first > 0) {
-            was[w] = (w == 0 ? a.p.ks : a.p.vs)[head];
-            scale[w] = fmaxf(scale[w], was[w]);
-        }
+        if (first > 0) scale[w] = fmaxf(scale[w], was[w]);
+        else was[w] = scale[w];
     }
     if (live && ok) {
         const float inv = 1.0f / scale[which];             // a power of two: exact
@@ -266,28 +283,30 @@ __global__ __launch_bounds__(NT) void append8_kernel(Append8 a) {
     }
     __syncthreads();
     if (ok) {
-        // the values' tile, a wave the four slots 4 q .. 4 q + 3; slots outside the unit keep their codes (rounded again
-        // where they came before it and the scale grew)
-        constexpr int W = HD / 64;                         // words a lane
+        // the values' tile; slots outside the unit keep their codes (rounded again where they came before it and the scale
+        // grew)
         const bool again_v = scale[1] > was[1];
-        const int lane = tid % 64;
-        for (int q = tid / 64; q < 4; q += NT / 64) {
-            const int lo = max(first - 4 * q, 0), hi = min(first + n - 4 * q, 4);      // new slots of the four
-            if (hi <= 0 || (lo >= 4 && !again_v)) continue;
-            const uint32_t below = lo >= 4 ? 0xffffffffu : (1u << (8 * lo)) - 1;   // slots before the unit
-            const uint32_t fresh = lo >= 4 ? 0u : (hi >= 4 ? 0xffffffffu : (1u << (8 * hi)) - 1) & ~below;
-            uint32_t *dst = (uint32_t *)(vp + q * (4 * HD)) + W * lane;
+#pragma unroll
+        for (int k = 0; k < QUADS; ++k) {
+            const int q = quad_of(k), lo = max(first - 4 * q, 0), hi = min(first + n - 4 * q, 4);
+            if (q >= 4 || hi <= 0 || lo >= 4) continue;
+            const uint32_t below = (1u << (8 * lo)) - 1;           // slots before the unit
+            const uint32_t fresh = (hi == 4 ? 0xffffffffu : (1u << (8 * hi)) - 1) & ~below;
             const uint32_t *src = (const uint32_t *)(tile + q * (4 * HD)) + W * lane;
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 uint32_t w = src[j];
                 if (fresh != 0xffffffffu) {
-                    const uint32_t old = dst[j];
-                    const uint32_t kept = again_v ? rescale4(old, was[1] / scale[1]) : old;
-                    w = (w & fresh) | (kept & below) | (old & ~(fresh | below));
+                    const uint32_t kept = again_v ? rescale4(old[k][j], was[1] / scale[1]) : old[k][j];
+                    w = (w & fresh) | (kept & below) | (old[k][j] & ~(fresh | below));
                 }
-                dst[j] = w;
+                words_of(q)[j] = w;
             }
+        }
+        if (again_v) {
+            for (int q = wave; q < first / 4; q += NT / 64)
+#pragma unroll
+                for (int j = 0; j < W; ++j) words_of(q)[j] = rescale4(words_of(q)[j], was[1] / scale[1]);
         }
         if (scale[0] > was[0]) {
             uint32_t *dst = (uint32_t *)kp;
