@@ -17,7 +17,7 @@ from paper_2609_25405_amd import _abi as A
 from paper_2609_25405_amd import ops
 from paper_2609_25405_amd import runtime as R
 from tests.parity import TOL, TOL_STATE, assert_vectors_close
-from workload import Batch, DecodeRow, EmbChunk, GenChunk, as_float64, draw_tokens, make_weights, tiny_config
+from workload import Batch, DecodeRow, EmbChunk, GenChunk, as_float64, draw_tokens, make_lora, make_weights, tiny_config
 
 pytestmark = pytest.mark.gpu
 PAGE = 16
@@ -53,9 +53,11 @@ class Held(OracleKV):
 class Served:
     """Models, caches and states of a run, stepped on the device and by the oracle."""
 
-    def __init__(self, dtype, two_models=False, two_caches=False, n_seq=8, max_blocks=24, max_tokens=700, cfg=None):
+    def __init__(self, dtype, two_models=False, two_caches=False, n_seq=8, max_blocks=24, max_tokens=700, cfg=None, lora=0):
         cfg = self.cfg = cfg or tiny_config(dtype).replace(n_kv_heads=2)
         self.W = [make_weights(cfg, 301), make_weights(cfg, 302, model_tag=1) if two_models else None]
+        if lora:
+            self.W[0]["adapters"] = [make_lora(cfg, 303, 16, tag=t) for t in range(lora)]
         self.dm = [R.DeviceModel(cfg, self.W[0])]
         self.dm.append(R.DeviceModel(cfg, self.W[1]) if two_models else self.dm[0])
         e = (cfg, as_float64(self.W[0]))
@@ -80,12 +82,12 @@ class Served:
         self.acc_w = torch.zeros(n_seq, device="cuda")
         self.ws = ops.WorkspaceKV8(*self.dm, max_tokens, 8, 8, max_blocks * PAGE)
 
-    def enqueue(self, batch, stream=None):
+    def enqueue(self, batch, stream=None, hidden=None):
         """(logits, sampled tokens, their scores, embeddings) of one step."""
         nc, nd = len(batch.chunks), batch.n_logit_rows
         logits = torch.full((max(1, nd), self.cfg.vocab), float("nan"), device="cuda")
         emb = torch.full((max(1, nc), self.cfg.d_model), float("nan"), device="cuda")
-        ops.step_kv8(*self.dm, batch, *self.kv, self.acc_sum, self.acc_w, logits, emb, self.ws, stream=stream)
+        ops.step_kv8(*self.dm, batch, *self.kv, self.acc_sum, self.acc_w, logits, emb, self.ws, stream=stream, hidden=hidden)
         logits, tok = logits[:nd], torch.full((nd,), -1, dtype=torch.int32, device="cuda")
         out = dict(logprob=torch.zeros(nd, device="cuda"), entropy=torch.zeros(nd, device="cuda"),
                    rank=torch.full((nd,), -1, dtype=torch.int32, device="cuda"),
@@ -96,7 +98,10 @@ class Served:
         return logits, tok, out, emb
 
     def step(self, batch):
-        logits, tok, out, emb = self.enqueue(batch)
+        hidden = None
+        if batch.hidden_stride:
+            hidden = torch.full((self.kv[0].n_seq, batch.hidden_stride, self.cfg.d_model), float("nan"), device="cuda")
+        logits, tok, out, emb = self.enqueue(batch, hidden=hidden)
         torch.cuda.synchronize()
         assert self.ws.device_error() == 0
         held = [Held(self.cfg, kv, t) for kv, t in zip(self.kv, self.table)]
@@ -115,7 +120,9 @@ class Served:
                 assert int(out["rank"][i]) == rank == 0 and out["top_ids"][i].tolist() == ids.tolist()
                 assert np.abs(out["top_logprobs"][i].double().cpu().numpy() - top).max() <= b
         for i, c in enumerate(batch.chunks):
-            if c.last:
+            if c.pool == "buffer":
+                assert_vectors_close(hidden[c.seq, c.offset:c.offset + c.len].cpu().numpy(), ref["hidden"][i], dt, "buffered rows")
+            elif c.last:
                 assert_vectors_close(emb[i].cpu().numpy(), ref["out_emb"][i], dt, "embedding")
             else:
                 assert torch.isnan(emb[i]).all()
@@ -165,6 +172,18 @@ def test_projection_in_two_parts(two):
     m.step(batch_of(m.cfg.vocab, 2, [], [], [DecodeRow(3, 40), DecodeRow(5, 3)], a))
 
 
+@pytest.mark.parametrize("dtype,two", [("bf16", False), ("f32", True)])
+def test_adapters_and_buffered_rows(dtype, two):
+    m = Served(dtype, two, two, lora=2)
+    b = batch_of(m.cfg.vocab, 1, [EmbChunk(0, 0, 23, False, "buffer"), EmbChunk(1, 0, 40, True, "mean"), EmbChunk(2, 0, 9, True, "last")],
+                 [GenChunk(3, 0, 21, True)])
+    b.chunk_adapter, b.hidden_stride = [1, 0, -1], 64
+    a = m.step(b)
+    b = batch_of(m.cfg.vocab, 2, [EmbChunk(0, 23, 30, True, "buffer")], [], [DecodeRow(3, 21)], a)
+    b.chunk_adapter, b.hidden_stride = [1], 64
+    m.step(b)
+
+
 def drawn_steps(v):
     yield batch_of(v, 1, [EmbChunk(0, 0, 20, False, "mean")], [GenChunk(3, 0, 40, True), GenChunk(4, 0, 18, True)])
     for i in range(4):
@@ -193,6 +212,38 @@ def test_steps_back_to_back_and_on_another_stream(two):
     for other in got[1:]:
         for x, y in zip(got[0], other):
             assert all(torch.equal(p, q) for p, q in zip(x, y))
+
+
+@pytest.mark.parametrize("two", [False, True])
+def test_threads_that_share_a_model(two):
+    """Two threads, each with caches, states, a workspace and a stream of its own, step the same models at once."""
+    import threading
+    m = Served("bf16", two, two)
+    want = [[x.cpu() for x in m.enqueue(b)[:2]] for b in drawn_steps(m.cfg.vocab)]
+    others, got, failed = [Served("bf16", two, two) for _ in range(2)], [[], []], []
+    for o in others:
+        o.dm = m.dm
+        o.stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def run(i):
+        try:
+            with torch.cuda.stream(others[i].stream):
+                outs = [others[i].enqueue(b)[:2] for b in drawn_steps(m.cfg.vocab)]
+            others[i].stream.synchronize()
+            got[i] = [[x.cpu() for x in o] for o in outs]
+        except Exception as e:          # reported by the main thread
+            failed.append(e)
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed, failed
+    for i in range(2):
+        assert others[i].ws.device_error() == 0
+        assert all(torch.equal(p, q) for x, y in zip(want, got[i]) for p, q in zip(x, y)) and len(got[i]) == len(want)
 
 
 def test_bad_page_is_flagged_and_other_rows_keep_their_results():
