@@ -10,7 +10,7 @@
 // + 7, two 16-byte loads of bf16, so that the pairs (i, i + HD / 2) of a head that turns whole, and
 // the pairs (2 i, 2 i + 1), are in one lane; pairs of a head that turns in part meet through LDS.
 //
-// Bound by the rows' bytes: 8.8 k bf16 rows of 32 + 2 x 8 heads of 128 dims in 47 us, 4.2 TB/s of 110 MB read and 90
+// Bound by the rows' bytes: 8.8 k bf16 rows of 32 + 2 x 8 heads of 128 dims in 42 us, 4.7 TB/s of 110 MB read and 90
 // written; 256 decode rows with norms in 7.0 us, one round of waves that wait for two dependent reads.  The read-back of the
 // same rows takes 14.7 and 5.6 us (18 MB in, 36 out).
 #include <type_traits>
@@ -101,6 +101,10 @@ __global__ __launch_bounds__(NT) void append8_kernel(Append8 a) {
     const bool ok = page >= 0 && page < a.p.n_pages;
     if (!ok && tid == 0) flag_error(a.p.err, ORTHRUS_DEVERR_PAGE);
 
+    // a thread's pair, the same for each of its tokens; its turns are read ahead of the rows, for which loads return in order
+    constexpr int PAIRS = HD / 2;
+    const int half = a.rot / 2, pair = tid % PAIRS;
+    const double rate = ((const double *)(a.p.meta + kTurnsInt))[min(pair, max(half - 1, 0))];
     const int grp = tid / LPR, i = tid % LPR;
     // head row `h` of token t: this lane's 16 dims (x[0]: 8 i .., x[1]: HD / 2 + 8 i ..)
     auto load_row = [&](int t, int h, float (&x)[2][8]) {
@@ -151,19 +155,15 @@ __global__ __launch_bounds__(NT) void append8_kernel(Append8 a) {
         }
     }
 
-    const int half = a.rot / 2;
-    if (half > 0) {
-        const double *turns = (const double *)(a.p.meta + kTurnsInt);
-        for (int k = tid; k < n * half; k += NT) {
-            const int tk = k / half, pr = k % half;
-            // turns modulo one in double: far positions keep their angle
-            const double c = (double)(block * kPage8 + first + tk) * turns[pr];
-            const double r = 2.0 * (c - rint(c));
-            const float f = (float)r, rest = (float)(r - (double)f) * (float)M_PI;     // what fp32 leaves of the angle
-            float sn, cs;
-            sincospif(f, &sn, &cs);
-            turn[tk][pr] = float2{fmaf(-sn, rest, cs) * a.magnitude, fmaf(cs, rest, sn) * a.magnitude};
-        }
+    for (int tk = tid / PAIRS; tk < n; tk += NT / PAIRS) {
+        if (pair >= half) break;
+        // turns modulo one in double: far positions keep their angle
+        const double c = (double)(block * kPage8 + first + tk) * rate;
+        const double r = 2.0 * (c - rint(c));
+        const float f = (float)r, rest = (float)(r - (double)f) * (float)M_PI;     // what fp32 leaves of the angle
+        float sn, cs;
+        sincospif(f, &sn, &cs);
+        turn[tk][pair] = float2{fmaf(-sn, rest, cs) * a.magnitude, fmaf(cs, rest, sn) * a.magnitude};
     }
     __syncthreads();
 
