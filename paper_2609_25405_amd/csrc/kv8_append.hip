@@ -11,8 +11,8 @@
 // the pairs (2 i, 2 i + 1), are in one lane; pairs of a head that turns in part meet through LDS.
 //
 // Bound by the rows' bytes: 8.8 k bf16 rows of 32 + 2 x 8 heads of 128 dims in 42 us, 4.7 TB/s of 110 MB read and 90
-// written; 256 decode rows with norms in 7.0 us, one round of waves that wait for two dependent reads.  The read-back of the
-// same rows takes 14.7 and 5.6 us (18 MB in, 36 out).
+// written; 256 decode rows with norms in 6.8 us, one round of waves that wait for two dependent reads.  The read-back of the
+// same rows takes 13.0 and 5.0 us (18 MB in, 36 out).
 #include <type_traits>
 
 #include "kv8.hpp"
@@ -349,34 +349,42 @@ template <int HD, int NT> __global__ __launch_bounds__(NT) void read8_kernel(Rea
     if (!ok && tid == 0) flag_error(a.p.err, ORTHRUS_DEVERR_PAGE);
     const size_t head = (size_t)(ok ? page : 0) * a.p.nkv + g;
     const uint8_t *kp = a.p.k + head * (kPage8 * HD), *vp = a.p.v + head * (kPage8 * HD);
+    // 16 threads a token, each PT dims of its key (and value, from the page's tile in LDS)
+    static_assert(NT == 64 || NT == 16 * kPage8, "a unit's tokens in one round");
+    const int t = tid / 16, d0 = (tid % 16) * PT, slot = first + t;
+    const bool live = t < n;
+    uint32_t kw[PT / 4] = {};
+    if (live && ok) {
+#pragma unroll
+        for (int j = 0; j < PT / 4; ++j) kw[j] = *(const uint32_t *)(kp + slot * HD + d0 + 4 * j);
+    }
     for (int i = tid; i < kPage8 * HD / 8; i += NT) ((uint2 *)tile)[i] = ((const uint2 *)vp)[i];
-    __syncthreads();
     const float ks = ok ? a.p.ks[head] : 1.f, vs = ok ? a.p.vs[head] : 1.f;
-    const int d0 = (tid % 16) * PT;
-    for (int t = tid / 16; t < n; t += NT / 16) {
-        const int slot = first + t;
-        uint32_t ow[2][PT / 2];
+    __syncthreads();
+    if (!live) return;
+    uint32_t ow[2][PT / 2];
 #pragma unroll
-        for (int j = 0; j < PT / 4; ++j) {
-            const uint2 w = word_bf16(ok ? *(const uint32_t *)(kp + slot * HD + d0 + 4 * j) : 0u, ks);
-            ow[0][2 * j] = w.x;
-            ow[0][2 * j + 1] = w.y;
-            uint32_t c = 0;
+    for (int j = 0; j < PT / 4; ++j) {
+        const uint2 w = word_bf16(kw[j], ks);
+        ow[0][2 * j] = w.x;
+        ow[0][2 * j + 1] = w.y;
+        uint32_t c = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int d = d0 + 4 * j + e;
-                c |= (uint32_t)tile[(slot / 4) * (4 * HD) + (d % 16) * (4 * DB) + (d / 16) * 4 + slot % 4] << (8 * e);
-            }
-            const uint2 v = word_bf16(ok ? c : 0u, vs);
-            ow[1][2 * j] = v.x;
-            ow[1][2 * j + 1] = v.y;
+        for (int e = 0; e < 4; ++e) {
+            const int d = d0 + 4 * j + e;
+            c |= (uint32_t)tile[(slot / 4) * (4 * HD) + (d % 16) * (4 * DB) + (d / 16) * 4 + slot % 4] << (8 * e);
         }
-        const size_t at = (size_t)(row0 + t) * ((size_t)a.p.nkv * HD) + (size_t)g * HD + d0;
-#pragma unroll
-        for (int j = 0; j < PT / 4; ++j) {
-            *(uint2 *)(a.k_out + at + 4 * j) = uint2{ow[0][2 * j], ow[0][2 * j + 1]};
-            *(uint2 *)(a.v_out + at + 4 * j) = uint2{ow[1][2 * j], ow[1][2 * j + 1]};
-        }
+        const uint2 v = word_bf16(ok ? c : 0u, vs);
+        ow[1][2 * j] = v.x;
+        ow[1][2 * j + 1] = v.y;
+    }
+    const size_t at = (size_t)(row0 + t) * ((size_t)a.p.nkv * HD) + (size_t)g * HD + d0;
+    if constexpr (PT == 8) {
+        *(u32x4 *)(a.k_out + at) = u32x4{ow[0][0], ow[0][1], ow[0][2], ow[0][3]};
+        *(u32x4 *)(a.v_out + at) = u32x4{ow[1][0], ow[1][1], ow[1][2], ow[1][3]};
+    } else {
+        *(uint2 *)(a.k_out + at) = uint2{ow[0][0], ow[0][1]};
+        *(uint2 *)(a.v_out + at) = uint2{ow[1][0], ow[1][1]};
     }
 }
 
