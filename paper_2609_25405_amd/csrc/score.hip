@@ -257,18 +257,24 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
     const int v0 = (int)((int64_t)slice * nvec / slices), v1 = (int)((int64_t)(slice + 1) * nvec / slices);
     const int tok = a.tokens ? a.tokens[row] : -1;
     const bool has = tok >= 0 && tok < a.vocab;
-    float v[E];
+    // Vectors [qa, qb) lie wholly in the row.  One before and one after them may lie in it in part: a thread of wave 1 and one
+    // of wave 2 take these as four entries more, read first; the other loads then stand in no branch, so that the first are
+    // used while the last are on their way (in branches each use waits for all: 256 rows of 32000 entries 12.7 us).
+    const int qa = off > 0, qb = (a.vocab + off) / 4;
+    const bool head = wave == 1 && off > 0 && slice == 0, tail = wave == 2 && qb >= v0 && qb < v1 && !(qb == 0 && off > 0);
+    const int ex = head ? -off : 4 * qb - off;
+    float v[E + 4];
 #pragma unroll
-    for (int i = 0; i < EV; ++i) {
-        const int q = v0 + i * NT + tid, e = 4 * q - off;
-        if (q < v1 && e >= 0 && e + 3 < a.vocab) {
-            const float4 f = *(const float4 *)(x + e);
+    for (int j = 0; j < 4; ++j) v[E + j] = (head || tail) && lane == 0 && ex + j >= 0 && ex + j < a.vocab ? x[ex + j] : -INFINITY;
+    const int whole0 = max(v0, qa), whole1 = min(v1, qb);
+    if (qb > qa) {
+#pragma unroll
+        for (int i = 0; i < EV; ++i) {
+            const float4 f = *(const float4 *)(x + (4 * min(max(v0 + i * NT + tid, qa), qb - 1) - off));
             v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[4 * i + j] = q < v1 && e + j >= 0 && e + j < a.vocab ? x[e + j] : -INFINITY;
         }
     }
+    auto entry_of = [&](int vec) { return vec < EV ? 4 * (v0 + vec * NT + tid) - off : ex; };
     const float xt = has ? x[tok] : INFINITY;
     if (tid == 0) sh.n_cand = 0;
     if (tid < 64) sh.larger[tid] = 0;
@@ -278,11 +284,10 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
     const uint32_t tb = __float_as_uint(xt);
     const float below = xt > 0.f ? __uint_as_float(tb - 1) : xt < 0.f ? __uint_as_float(tb + 1) : __uint_as_float(0x80000001u);
     int before = 0;
-#pragma unroll
-    for (int c = 0; c < E; c += CH) {
+    auto take = [&](int c, int count) {
         float mc = v[c];
 #pragma unroll
-        for (int j = 1; j < CH; ++j) mc = fmaxf(mc, v[c + j]);
+        for (int j = 1; j < count; ++j) mc = fmaxf(mc, v[c + j]);
         if (mc > top) {
             top = mc;
             const float r1 = mc * kL, f = __builtin_amdgcn_exp2f(r0 - r1);
@@ -291,15 +296,15 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
             r0 = r1;
         }
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
+        for (int j = 0; j < count; ++j) {
             const float t = fmaf(v[c + j], kL, -r0), w = __builtin_amdgcn_exp2f(t);
             z += w;
             s = fmaf(w, fmaxf(t, kLeastT), s);
         }
         if (has) {
 #pragma unroll
-            for (int i = c / 4; i < (c + CH) / 4; ++i) {
-                const int e = 4 * (v0 + i * NT + tid) - off;
+            for (int i = c / 4; i < (c + count) / 4; ++i) {
+                const int e = entry_of(i);
                 const float limit = e + 3 < tok ? below : xt;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) before += v[4 * i + j] > limit ? 1 : 0;
@@ -309,7 +314,21 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
                 }
             }
         }
+    };
+#pragma unroll
+    for (int c = 0; c < E; c += CH) {
+#pragma unroll
+        for (int i = c / 4; i < (c + CH) / 4; ++i) {
+            const int q = v0 + i * NT + tid;
+            const bool in = q >= whole0 && q < whole1;
+            if (__ballot(!in)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[4 * i + j] = in ? v[4 * i + j] : -INFINITY;
+            }
+        }
+        take(c, CH);
     }
+    if (head || tail) take(E, 4);
     float gm = top;
     if constexpr (GL >= 2) gm = fmaxf(gm, lane_xorf<1>(gm));
     if constexpr (GL >= 4) gm = fmaxf(gm, lane_xorf<2>(gm));
@@ -351,8 +370,8 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
         }
         if (top >= bound) {
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const int e = 4 * (v0 + i / 4 * NT + tid) - off + i % 4;
+            for (int i = 0; i < E + 4; ++i) {
+                const int e = entry_of(i / 4) + i % 4;
                 if (v[i] >= bound) {
                     const int c = atomicAdd(&sh.n_cand, 1);
                     if (c < kCands) sh.cand[c] = key_of(order_of(v[i]), e);
