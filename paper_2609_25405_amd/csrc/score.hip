@@ -93,6 +93,19 @@ __device__ __forceinline__ float wave_maxf(float v) {
     v = fmaxf(v, lane_xorf<16>(v));
     return fmaxf(v, lane_xorf<32>(v));
 }
+// the larger of two, not a number above all, and that of a wave
+__device__ __forceinline__ double larger_of(double a, double b) { return b > a || b != b ? b : a; }
+template <int M> __device__ __forceinline__ double lane_larger(double v) {
+    return larger_of(v, __builtin_bit_cast(double, lane_xor64<M>(__builtin_bit_cast(u64, v))));
+}
+__device__ __forceinline__ double wave_larger(double v) {
+    v = lane_larger<1>(v);
+    v = lane_larger<2>(v);
+    v = lane_larger<4>(v);
+    v = lane_larger<8>(v);
+    v = lane_larger<16>(v);
+    return lane_larger<32>(v);
+}
 __device__ __forceinline__ u64 reversed64(u64 v) {
     const int lane = 63 - (threadIdx.x & 63);
     return (u64)__shfl((uint32_t)(v >> 32), lane, 64) << 32 | __shfl((uint32_t)v, lane, 64);
@@ -137,11 +150,12 @@ struct Part {
 };
 __host__ __device__ __forceinline__ size_t part_bytes(int n_top) { return sizeof(Part) + 8 * (size_t)n_top; }
 
-__device__ void write_row(const Score &a, int r, int tok, const Part &p, u64 key, int lane) {
+// (xt: the token's logit, if it has one)
+__device__ void write_row(const Score &a, int r, int tok, float xt, const Part &p, u64 key, int lane) {
     const double logz = (p.r + (double)log2f(p.z)) / (double)kL;
     if (lane == 0) {
         const bool has = a.tokens && tok >= 0 && tok < a.vocab;
-        if (a.logprob) a.logprob[r] = has ? (float)((double)a.logits[(size_t)r * a.stride + tok] - logz) : NAN;
+        if (a.logprob) a.logprob[r] = has ? (float)((double)xt - logz) : NAN;
         if (a.rank) a.rank[r] = has ? p.rank : -1;
         if (a.entropy) a.entropy[r] = (log2f(p.z) - p.s / p.z) / kL;
     }
@@ -402,7 +416,7 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
         }
     }
     if (slices == 1) {
-        write_row(a, row, tok, p, key, lane);
+        write_row(a, row, tok, xt, p, key, lane);
         return;
     }
     char *pp = a.ws + (size_t)blockIdx.x * part_bytes(a.n_top);
@@ -415,29 +429,36 @@ __global__ __launch_bounds__(64) void score_merge_kernel(Score a, int slices) {
     const int r = blockIdx.x, lane = threadIdx.x;
     const char *pp = a.ws + (size_t)r * slices * part_bytes(a.n_top);
     auto part = [&](int s) { return (const Part *)(pp + s * part_bytes(a.n_top)); };
-    Part p{-INFINITY, 0.f, 0.f, 0, 0};
-    for (int s = 0; s < slices; ++s) {
-        const double r = part(s)->r;
-        p.r = r > p.r || r != r ? r : p.r;
-    }
-    for (int s = 0; s < slices; ++s) {
-        const Part q = *part(s);
+    const int total = slices * a.n_top;
+    auto key_at = [&](int i) { return i < total ? ((const u64 *)(part(i / a.n_top) + 1))[i % a.n_top] : 0; };
+    // a lane a slice (and every 64th after it); all that a few slices left is on its way at once
+    const Part none{-INFINITY, 0.f, 0.f, 0, 0};
+    Part q = lane < slices ? *part(lane) : none, p = none;
+    const u64 first_key = key_at(lane);
+    const int tok = a.tokens ? a.tokens[r] : -1;
+    const float xt = tok >= 0 && tok < a.vocab ? a.logits[(size_t)r * a.stride + tok] : 0.f;
+    p.r = q.r;
+    for (int s = lane + 64; s < slices; s += 64) p.r = larger_of(p.r, part(s)->r);
+    p.r = wave_larger(p.r);
+    for (int s = lane; s < slices; s += 64) {
+        if (s > lane) q = *part(s);
         p.rank += q.rank;
         if (q.r == -INFINITY) continue;                // nothing but -inf in the slice
         const float d = (float)(q.r - p.r), f = __builtin_amdgcn_exp2f(d);
         p.z += q.z * f;
         p.s += f * (q.s + q.z * fmaxf(d, kLeastT));
     }
+    p.z = wave_addf(p.z);
+    p.s = wave_addf(p.s);
+    p.rank = wave_addi(p.rank);
     if (p.r == -INFINITY) p.z = NAN;
     u64 key = 0;
-    const int total = slices * a.n_top;
     for (int c = 0; c < total; c += 64) {
-        const int i = c + lane;
-        const u64 k = i < total ? ((const u64 *)(part(i / a.n_top) + 1))[i % a.n_top] : 0;
+        const u64 k = c == 0 ? first_key : key_at(c + lane);
         const u64 sorted = wave_sort(k, lane);
         key = c == 0 ? sorted : wave_merge(key, reversed64(sorted), lane);
     }
-    write_row(a, r, a.tokens ? a.tokens[r] : -1, p, key, lane);
+    write_row(a, r, tok, xt, p, key, lane);
 }
 
 }  // namespace
