@@ -1,14 +1,14 @@
 // Scores of tokens under logits: log probability, entropy, rank and the largest entries of each row.
 //
 // A row is read once: a workgroup holds its slice of up to kSliceMost entries in registers, so the maximum is
-// known before the first exponential and nothing is rescaled (1999 rows of 131072 entries 173 us, 6.0 TB/s; 256 rows
-// of 32000 with 20 alternatives 11.7 us).  Longer rows are several slices, joined by a
+// known before the first exponential and nothing is rescaled (1999 rows of 131072 entries 171 us, 6.1 TB/s; 256 rows
+// of 32000 with 20 alternatives 11.4 us).  Longer rows are several slices, joined by a
 // second launch of one wave a row.
 //
 // Order.  An entry's key is its value as an order-preserving integer (NaN above everything, -0 equal to +0) over the
 // complement of its index, so all keys differ and equal values rank by index.
 // The n largest of a slice: the n-th largest of the maxima of 64 groups of threads is a bound that n entries reach;
-// the few that reach it (24 on average for n = 20) go to LDS as keys and one wave sorts them.
+// the few that reach it (24 on average for n = 20) go to LDS as keys and one wave puts them in order.
 // Rank: entries of a lower index count where they are not smaller than the token's, the others where they are larger.
 //
 // Slices with a NaN, an infinite maximum, more candidates than LDS holds (long ties) or a token whose own logit is not
@@ -398,9 +398,10 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
     }
     Part p{(double)r, block_total<NT>(sh.red[0]), 0.f, 0, 0};
     u64 key = 0;
-    const int nc = sh.n_cand;
+    const int nc = __builtin_amdgcn_readfirstlane(sh.n_cand);
     // (block-uniform: every thread has read the same sums)
-    if (!(p.z > 0.f && p.z < INFINITY) || (has && !(fabsf(xt) < INFINITY)) || nc > kCands || nc < a.n_top) {
+    const bool odd = !(p.z > 0.f && p.z < INFINITY) || (has && !(fabsf(xt) < INFINITY)) || nc > kCands || nc < a.n_top;
+    if (__builtin_expect(odd, false)) {
         slice_by_keys<NT>(sh, x, max(4 * v0 - off, 0), min(4 * v1 - off, a.vocab), a.n_top, has, tok, slices == 1, p, key);
         if (wave != 0) return;
     } else {
@@ -408,7 +409,18 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
         p.s = block_total<NT>(sh.red[1]);
 #pragma unroll
         for (int w = 0; w < NW; ++w) p.rank += sh.red_rank[w];
-        if (a.n_top > 0) {
+        if (a.n_top > 0 && nc <= 64) {
+            // a candidate's place is the number of larger ones (1999 rows of 131072 entries 175 us with a sort, 171)
+            const u64 mine = lane < nc ? sh.cand[lane] : 0;
+            int place = 0;
+#pragma unroll 8
+            for (int o = 0; o < nc; ++o) place += sh.cand[o] > mine ? 1 : 0;
+            if (lane < nc) sh.cand[64 + place] = mine;
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            key = lane < nc ? sh.cand[64 + lane] : 0;
+        } else if (a.n_top > 0) {
             for (int c = 0; c < nc; c += 64) {
                 const u64 k = wave_sort(c + lane < nc ? sh.cand[c + lane] : 0, lane);
                 key = c == 0 ? k : wave_merge(key, reversed64(k), lane);
