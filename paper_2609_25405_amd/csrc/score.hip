@@ -17,7 +17,7 @@
 
 #include "score.hpp"
 
-// a reference r = L x is the rounded product wherever it is used: no contraction but the written fused operations
+// a weight's exponent is a rounded difference times L wherever it is taken: no contraction but the written fused operations
 #pragma clang fp contract(off)
 
 namespace orthrus {
@@ -94,11 +94,9 @@ __device__ __forceinline__ float wave_maxf(float v) {
     return fmaxf(v, lane_xorf<32>(v));
 }
 // the larger of two, not a number above all, and that of a wave
-__device__ __forceinline__ double larger_of(double a, double b) { return b > a || b != b ? b : a; }
-template <int M> __device__ __forceinline__ double lane_larger(double v) {
-    return larger_of(v, __builtin_bit_cast(double, lane_xor64<M>(__builtin_bit_cast(u64, v))));
-}
-__device__ __forceinline__ double wave_larger(double v) {
+__device__ __forceinline__ float larger_of(float a, float b) { return b > a || b != b ? b : a; }
+template <int M> __device__ __forceinline__ float lane_larger(float v) { return larger_of(v, lane_xorf<M>(v)); }
+__device__ __forceinline__ float wave_larger(float v) {
     v = lane_larger<1>(v);
     v = lane_larger<2>(v);
     v = lane_larger<4>(v);
@@ -136,32 +134,35 @@ __device__ __forceinline__ u64 wave_merge(u64 mine, u64 other_reversed, int lane
     return wave_stage<64>(mine > other_reversed ? mine : other_reversed, lane);
 }
 
-// Sums are held in base 2^L, L = log2(e) as an fp32 number: with a reference r near L max x, z = sum 2^(L x - r) and
-// s = sum (L x - r) 2^(L x - r), so that log Z = (r + log2 z) / L and the entropy is (log2 z - s / z) / L whatever r's own
-// rounding; L x - r is one fused operation.  What L differs from log2(e) by is a factor 1 + 1.3e-8 on the logits.
+// Sums are held in base 2^L, L = log2(e) as an fp32 number, under a reference m that is one of the entries: with
+// t = (x - m) L, z = sum 2^t and s = sum t 2^t, log Z = m + log2(z) / L and the entropy is (log2 z - s / z) / L.  The difference
+// x - m is taken first, and a token's log probability as (x - m) - log2(z) / L, so that no size of the logits costs
+// digits: of L x - r for a rounded r = L m, r's own rounding is left, 2^6 and more from logits of 1e9 on.  What L differs from
+// log2(e) by is a factor 1 + 1.3e-8 on the differences.
 constexpr float kL = 1.4426950408889634f;
+constexpr float kNoTop = -3.4028234663852886e38f;      // the reference before any entry: the least finite number
 constexpr float kLeastT = -300.f;      // exponents below it weigh nothing, and minus infinity must not meet that zero
 
 // what a slice leaves to the merge launch, in the workspace: one Part, then n_top keys
 struct Part {
-    double r;      // L times a finite maximum, or the maximum (not finite)
-    float z, s;
-    int rank, pad;
+    float m, z, s;      // the maximum and the sums under it
+    int rank;
 };
 __host__ __device__ __forceinline__ size_t part_bytes(int n_top) { return sizeof(Part) + 8 * (size_t)n_top; }
 
 // (xt: the token's logit, if it has one)
 __device__ void write_row(const Score &a, int r, int tok, float xt, const Part &p, u64 key, int lane) {
-    const double logz = (p.r + (double)log2f(p.z)) / (double)kL;
+    const double logz = (double)log2f(p.z) * (1.0 / (double)kL);         // beside the maximum
+    auto log_probability = [&](float v) { return (float)(((double)v - (double)p.m) - logz); };
     if (lane == 0) {
         const bool has = a.tokens && tok >= 0 && tok < a.vocab;
-        if (a.logprob) a.logprob[r] = has ? (float)((double)xt - logz) : NAN;
+        if (a.logprob) a.logprob[r] = has ? log_probability(xt) : NAN;
         if (a.rank) a.rank[r] = has ? p.rank : -1;
         if (a.entropy) a.entropy[r] = (log2f(p.z) - p.s / p.z) / kL;
     }
     if (lane < a.n_top) {
         if (a.top_ids) a.top_ids[(size_t)r * a.n_top + lane] = index_of(key);
-        if (a.top_logprobs) a.top_logprobs[(size_t)r * a.n_top + lane] = (float)((double)value_of((uint32_t)(key >> 32)) - logz);
+        if (a.top_logprobs) a.top_logprobs[(size_t)r * a.n_top + lane] = log_probability(value_of((uint32_t)(key >> 32)));
     }
 }
 
@@ -250,7 +251,7 @@ __device__ void slice_by_keys(ScoreShared<NT> &sh, const float *x, int e0, int e
         if (last == 0) break;              // fewer entries than n
     }
     __syncthreads();
-    p.r = (double)m * (double)kL;
+    p.m = m;
     p.z = block_total<NT>(sh.red[0]);
     p.s = block_total<NT>(sh.red[1]);
     p.rank = 0;
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
     if (tid == 0) sh.n_cand = 0;
     if (tid < 64) sh.larger[tid] = 0;
     // eight entries at a time, as they arrive, under a reference of the thread's own
-    float top = -1e37f, z = 0.f, s = 0.f, r0 = -1e37f * kL;
+    float top = kNoTop, z = 0.f, s = 0.f;
     // entries before the token: the next smaller float turns "not smaller" into "larger"
     const uint32_t tb = __float_as_uint(xt);
     const float below = xt > 0.f ? __uint_as_float(tb - 1) : xt < 0.f ? __uint_as_float(tb + 1) : __uint_as_float(0x80000001u);
@@ -303,15 +304,14 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
 #pragma unroll
         for (int j = 1; j < count; ++j) mc = fmaxf(mc, v[c + j]);
         if (mc > top) {
-            top = mc;
-            const float r1 = mc * kL, f = __builtin_amdgcn_exp2f(r0 - r1);
-            s = f * fmaf(z, r0 - r1, s);
+            const float d = (top - mc) * kL, f = __builtin_amdgcn_exp2f(d);
+            s = f * fmaf(z, fmaxf(d, kLeastT), s);
             z *= f;
-            r0 = r1;
+            top = mc;
         }
 #pragma unroll
         for (int j = 0; j < count; ++j) {
-            const float t = fmaf(v[c + j], kL, -r0), w = __builtin_amdgcn_exp2f(t);
+            const float t = (v[c + j] - top) * kL, w = __builtin_amdgcn_exp2f(t);
             z += w;
             s = fmaf(w, fmaxf(t, kLeastT), s);
         }
@@ -351,10 +351,10 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
     if (lane % GL == 0) sh.group[tid / GL] = gm;
     __syncthreads();
     gm = sh.group[lane];
-    const float m = wave_maxf(gm), r = m * kL;
+    const float m = wave_maxf(gm);
     {
-        const float f = __builtin_amdgcn_exp2f(r0 - r);
-        s = f * fmaf(z, fmaxf(r0 - r, kLeastT), s);
+        const float d = (top - m) * kL, f = __builtin_amdgcn_exp2f(d);
+        s = f * fmaf(z, fmaxf(d, kLeastT), s);
         z *= f;
     }
     z = wave_addf(z);
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void score_kernel(Score a, 
         }
         __syncthreads();
     }
-    Part p{(double)r, block_total<NT>(sh.red[0]), 0.f, 0, 0};
+    Part p{m, block_total<NT>(sh.red[0]), 0.f, 0};
     u64 key = 0;
     const int nc = __builtin_amdgcn_readfirstlane(sh.n_cand);
     // (block-uniform: every thread has read the same sums)
@@ -444,26 +444,26 @@ __global__ __launch_bounds__(64) void score_merge_kernel(Score a, int slices) {
     const int total = slices * a.n_top;
     auto key_at = [&](int i) { return i < total ? ((const u64 *)(part(i / a.n_top) + 1))[i % a.n_top] : 0; };
     // a lane a slice (and every 64th after it); all that a few slices left is on its way at once
-    const Part none{-INFINITY, 0.f, 0.f, 0, 0};
+    const Part none{-INFINITY, 0.f, 0.f, 0};
     Part q = lane < slices ? *part(lane) : none, p = none;
     const u64 first_key = key_at(lane);
     const int tok = a.tokens ? a.tokens[r] : -1;
     const float xt = tok >= 0 && tok < a.vocab ? a.logits[(size_t)r * a.stride + tok] : 0.f;
-    p.r = q.r;
-    for (int s = lane + 64; s < slices; s += 64) p.r = larger_of(p.r, part(s)->r);
-    p.r = wave_larger(p.r);
+    p.m = q.m;
+    for (int s = lane + 64; s < slices; s += 64) p.m = larger_of(p.m, part(s)->m);
+    p.m = wave_larger(p.m);
     for (int s = lane; s < slices; s += 64) {
         if (s > lane) q = *part(s);
         p.rank += q.rank;
-        if (q.r == -INFINITY) continue;                // nothing but -inf in the slice
-        const float d = (float)(q.r - p.r), f = __builtin_amdgcn_exp2f(d);
+        if (q.m == -INFINITY) continue;                // nothing but -inf in the slice
+        const float d = (q.m - p.m) * kL, f = __builtin_amdgcn_exp2f(d);
         p.z += q.z * f;
         p.s += f * (q.s + q.z * fmaxf(d, kLeastT));
     }
     p.z = wave_addf(p.z);
     p.s = wave_addf(p.s);
     p.rank = wave_addi(p.rank);
-    if (p.r == -INFINITY) p.z = NAN;
+    if (p.m == -INFINITY) p.z = NAN;
     u64 key = 0;
     for (int c = 0; c < total; c += 64) {
         const u64 k = c == 0 ? first_key : key_at(c + lane);
