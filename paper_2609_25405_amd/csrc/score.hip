@@ -231,11 +231,12 @@ __device__ void slice_by_keys(ScoreShared<NT> &sh, const float *x, int e0, int e
         sh.red_rank[wave] = before;
     }
     // n rounds: the largest key below the last one
-    u64 last = ~0ull;
+    u64 last = ~0ull;                      // (the first is below or at it: a NaN at index 0 has that key)
     key = 0;
     for (int i = 0; i < n; ++i) {
-        u64 mine = top < last ? top : 0;
-        if (top >= last && top != 0) {     // this thread's largest is taken: its next
+        const bool taken = i > 0 && top >= last && top != 0;
+        u64 mine = taken ? 0 : top;
+        if (taken) {                       // this thread's largest is taken: its next
             for (int e = e0 + tid; e < e1; e += NT) {
                 const u64 k = key_of(order_of(x[e]), e);
                 if (k < last && k > mine) mine = k;

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_logprobs import check
+from tests.test_gpu_logprobs import call, check
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +62,16 @@ def test_large_logits_close_together(vocab, base):
     x[0] = b - np.abs(np.spacing(b)) * rng.integers(0, 3, vocab).astype(np.float32)
     x[2, vocab // 2] = b - 64 * np.abs(np.spacing(b))
     check(torch.tensor(x, device="cuda"), tokens(vocab - 1, 0, vocab // 2), 5)
+
+
+@pytest.mark.parametrize("vocab", [5, 1003, 20000, 66000])
+def test_a_row_whose_first_logit_is_not_a_number(vocab):
+    x = torch.randn((3, vocab), device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    x[0, 0] = float("nan")
+    x[1, 0], x[1, 3] = -float("nan"), float("nan")
+    o = call(x, tokens(0, 3, 0), 3)
+    rest = x[0].cpu().numpy().copy()
+    rest[0] = -np.inf
+    assert o["top_ids"][0].tolist() == [0] + np.argsort(-rest, kind="stable")[:2].tolist()
+    assert o["top_ids"][1][:2].tolist() == [0, 3] and o["rank"].tolist()[:2] == [0, 1]
+    assert np.isnan(o["logprob"][:2]).all() and np.isfinite(o["logprob"][2])
