@@ -171,7 +171,7 @@ constexpr int kCands = 1024;
 template <int NT> struct ScoreShared {
     static constexpr int NW = NT / 64;
     u64 cand[kCands];
-    u64 best[NT];                 // slice_by_keys
+    u64 best[NW];                 // slice_by_keys
     float group[64];
     int larger[64];
     float red[2][NW];
@@ -186,9 +186,8 @@ template <int NT> __device__ __forceinline__ float block_total(const float *red)
     return t;
 }
 
-// The slice [e0, e1) of row x by keys alone: every thread's largest key, the 64 largest of those (sorted in each wave, merged
-// over the waves), whose n-th is a bound; the at most 64 threads that reach it then pass their keys in
-// descending order, one at a time.
+// The slice [e0, e1) of row x by keys alone: the sums under the largest, then the n largest one at a time, each the largest of
+// what the threads have next.
 template <int NT>
 __device__ void slice_by_keys(ScoreShared<NT> &sh, const float *x, int e0, int e1, int n, bool has, int tok, bool alone, Part &p,
                               u64 &key) {
@@ -202,18 +201,16 @@ __device__ void slice_by_keys(ScoreShared<NT> &sh, const float *x, int e0, int e
         top = k > top ? k : top;
         before += has && k > tok_key ? 1 : 0;
     }
-    __syncthreads();              // the fast path is done with what follows
-    u64 sorted = wave_sort(top, lane);
-    sh.best[tid] = sorted;
-    for (int half = NW / 2; half >= 1; half /= 2) {
+    auto largest_of = [&](u64 mine) {      // the workgroup's largest (its first barrier: the fast path is done with what follows)
+        mine = wave_max64(mine);
         __syncthreads();
-        if (wave < half) {
-            sorted = wave_merge(sorted, sh.best[(wave + half) * 64 + 63 - lane], lane);
-            sh.best[tid] = sorted;
-        }
-    }
-    __syncthreads();
-    const float m = value_of((uint32_t)(sh.best[0] >> 32));
+        if (lane == 0) sh.best[wave] = mine;
+        __syncthreads();
+        u64 all = 0;
+        for (int w = 0; w < NW; ++w) all = sh.best[w] > all ? sh.best[w] : all;
+        return all;
+    };
+    const float m = value_of((uint32_t)(largest_of(top) >> 32));
     const bool none = m == -INFINITY;      // nothing but -inf in the slice
     float z = 0.f, s = 0.f;
     for (int e = e0 + tid; e < e1; e += NT) {
@@ -242,12 +239,7 @@ __device__ void slice_by_keys(ScoreShared<NT> &sh, const float *x, int e0, int e
                 if (k < last && k > mine) mine = k;
             }
         }
-        mine = wave_max64(mine);
-        __syncthreads();
-        if (lane == 0) sh.best[wave] = mine;
-        __syncthreads();
-        last = 0;
-        for (int w = 0; w < NW; ++w) last = sh.best[w] > last ? sh.best[w] : last;
+        last = largest_of(mine);
         if (lane == i) key = last;
         if (last == 0) break;              // fewer entries than n
     }
