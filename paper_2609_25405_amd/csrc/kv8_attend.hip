@@ -120,6 +120,31 @@ __device__ __forceinline__ bool has_key(const Attend8 &a, int at, int row) {
     return false;
 }
 
+// The last position among the keys of the item at `at` of the plan that not all of its rows see, whose value is not finite (-1:
+// none); by one wave.  Sums that are not finite for another reason are what they should be.
+template <int HD> __device__ int last_odd_value(const Attend8 &a, int at) {
+    const int32_t *it = a.p.meta + at, *table = a.p.table + (size_t)it[A8_SEQ] * a.p.max_blocks;
+    const int first = max(it[A8_KEY0], it[A8_POS] + 1), end = it[A8_KEY1], lane = threadIdx.x & 63;
+    int found = -1;
+    for (int b = first / kPage8; b * kPage8 < end; ++b) {
+        const int id = table[b];
+        if (id < 0 || id >= a.p.n_pages) continue;
+        const size_t head = (size_t)id * a.p.nkv + it[A8_HEAD];
+        const uint32_t *words = (const uint32_t *)(a.p.v + head * (kPage8 * HD));
+        const bool all = !(fabsf(a.p.vs[head]) * 448.f < INFINITY);
+        for (int i = lane; i < kPage8 * HD / 4; i += 64) {            // four slots of a dim
+            const uint32_t w = words[i];
+            for (int e = 0; e < 4; ++e) {
+                const int pos = b * kPage8 + i / HD * 4 + e;
+                if (pos >= first && pos < end && (all || (w >> (8 * e) & 0x7f) == 0x7f)) found = max(found, pos);
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) found = max(found, __shfl_xor(found, o, 64));
+    return found;
+}
+
 // One (row, query head) pair, by one wave, key after key, so that nothing the row does not see enters its
 // sums: for pairs whose sums met something not finite in a masked place (zero times it is not zero).
 // Lane l holds dims l (and l + 64).
@@ -435,6 +460,7 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
     // pairs of an earlier row of several: a later row's key or value that is not finite is masked, not absent
     if (len > 1) {
         __syncthreads();       // after the stores above, which it may replace
+        int last_odd = -2;     // (not looked for)
         for (int col = wave; col < cols; col += NW) {
             bool bad = false;
 #pragma unroll
@@ -443,6 +469,8 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
             if (__ballot(bad) == 0) continue;
             const int t = col / group, hh = g * group + col % group;
             if (pos0 + t + 1 >= key1) continue;        // nothing masked
+            if (last_odd == -2) last_odd = last_odd_value<HD>(a, a.off_small + kItem8Ints * index);
+            if (last_odd <= pos0 + t) continue;
             float o[HD / 64], mm, ll;
             pair_key_by_key<T, HD>(a, seq, g, pos0 + t, key0, key1, (const T *)a.q + (size_t)(row0 + t) * a.q_stride + (size_t)hh * HD, mm, ll, o);
             float *pp = partial_of<HD>(a, max(slot, 0), col);
@@ -795,7 +823,11 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int e = 0; e < 16; ++e) odd |= !(fabsf(acc[d][e]) < INFINITY);
-    const uint64_t oddb = __ballot(odd && c < cols && pos + 1 < key1);     // (a pair that sees every key has nothing masked)
+    uint64_t oddb = __ballot(odd && c < cols && pos + 1 < key1);     // (a pair that sees every key has nothing masked)
+    if (oddb) {
+        const int last_odd = last_odd_value<HD>(a, a.off_tiles + kItem8Ints * index);
+        oddb = __ballot(odd && c < cols && pos < last_odd);
+    }
     const uint32_t odd_cols = (uint32_t)oddb | (uint32_t)(oddb >> 32);
     for (int k = 0; k < 32; ++k) {
         if (!(odd_cols >> k & 1)) continue;
