@@ -100,7 +100,8 @@ int orthrus_rows_items(const orthrus_rows *r, const orthrus_kv8 *kv, const orthr
  * turns.  q_out: device [rows][q_stride] of the shape's dtype: the rotated query heads.  Keys (rotated) and
  * values are appended at the rows' positions.  Strides in elements, multiples of 8, at least
  * (n_q + 2 n_kv) head_dim and n_q head_dim; bases 16-byte aligned (EINVAL).  qkv_dtype ORTHRUS_BF16 needs a
- * shape of that dtype (EUNSUPPORTED).  A page id outside [0, n_pages) sets ORTHRUS_DEVERR_PAGE and its
+ * shape of that dtype (EUNSUPPORTED).  q_out may be the rows' own query columns (base, stride and type of qkv); else
+ * it shares no element with them.  A page id outside [0, n_pages) sets ORTHRUS_DEVERR_PAGE and its
  * tokens are not stored. */
 int orthrus_kv8_append(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer, const void *qkv, int32_t qkv_dtype,
                        int64_t row_stride, const float *q_gain, const float *k_gain, void *q_out, int64_t q_stride,
@@ -114,7 +115,8 @@ int orthrus_kv8_read(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer
  * sequence sees positions 0 .. p (its own key and value appended before); query head h reads KV
  * head h / (n_q / n_kv).  out = softmax(scale * q k^T) v; scale 0 means 1 / sqrt(head_dim) (EINVAL if
  * negative or not finite).  q, out: device [rows][stride] of the shape's dtype, n_q head_dim values a
- * row; strides multiples of 8 elements, bases 16-byte aligned (EINVAL).  Scores, softmax and sums in
+ * row; strides multiples of 8 elements, bases 16-byte aligned (EINVAL); out may be q itself (base and stride), else the
+ * two share no element.  Scores, softmax and sums in
  * fp32; bfloat16 rows round the softmax weights to bfloat16 before the product with the values, fp32 rows keep
  * them whole.  Keys of a page outside [0, n_pages) are skipped (ORTHRUS_DEVERR_PAGE); a row
  * left without keys is zero.  A row that sees only scores of minus infinity is not a number, as its softmax. */

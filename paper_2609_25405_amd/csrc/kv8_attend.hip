@@ -429,6 +429,35 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
     __syncthreads();
     int group = a.p.group;
     asm("" : "+v"(group));       // its reciprocal is taken anew: kept through the loop it would cost a spill
+    // Pairs of an earlier row of several: a later row's value that is not finite is masked, not absent.  Their sums are taken
+    // again here, ahead of any store to rows that may be q's own.
+    if (len > 1) {
+        int last_odd = -2;     // (not looked for)
+        for (int col = wave; col < cols; col += NW) {
+            bool bad = false;
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+                for (int d = lane; d < HD; d += 64) bad |= !(fabsf(sums(w, col)[d]) < INFINITY);
+            if (__ballot(bad) == 0) continue;
+            const int t = col / group, hh = g * group + col % group;
+            if (pos0 + t + 1 >= key1) continue;        // nothing masked
+            if (last_odd == -2) last_odd = last_odd_value<HD>(a, a.off_small + kItem8Ints * index);
+            if (last_odd <= pos0 + t) continue;
+            float o[HD / 64], mm, ll;
+            pair_key_by_key<T, HD>(a, seq, g, pos0 + t, key0, key1, (const T *)a.q + (size_t)(row0 + t) * a.q_stride + (size_t)hh * HD, mm, ll, o);
+            // as the first wave's sums, the others without keys
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                if (lane == 0) {
+                    sm[w * 16 + col] = w == 0 ? mm : -INFINITY;
+                    sl[w * 16 + col] = w == 0 && !(ll < 0.f) ? ll : 0.f;
+                }
+#pragma unroll
+                for (int d = 0; d < HD / 64; ++d) sums(w, col)[lane + 64 * d] = w == 0 ? o[d] : 0.f;
+            }
+        }
+        __syncthreads();
+    }
     // merge the waves in order; four dims a thread
     for (int o = tid; o < cols * (HD / 4); o += 64 * NW) {
         const int col = o / (HD / 4), d = o % (HD / 4) * 4;
@@ -455,34 +484,6 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
             const float inv = inverse(L);
             T *dst = (T *)a.out + (size_t)(row0 + col / group) * a.out_stride + (size_t)(g * group + col % group) * HD + d;
             store4(dst, sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv);
-        }
-    }
-    // pairs of an earlier row of several: a later row's key or value that is not finite is masked, not absent
-    if (len > 1) {
-        __syncthreads();       // after the stores above, which it may replace
-        int last_odd = -2;     // (not looked for)
-        for (int col = wave; col < cols; col += NW) {
-            bool bad = false;
-#pragma unroll
-            for (int w = 0; w < NW; ++w)
-                for (int d = lane; d < HD; d += 64) bad |= !(fabsf(sums(w, col)[d]) < INFINITY);
-            if (__ballot(bad) == 0) continue;
-            const int t = col / group, hh = g * group + col % group;
-            if (pos0 + t + 1 >= key1) continue;        // nothing masked
-            if (last_odd == -2) last_odd = last_odd_value<HD>(a, a.off_small + kItem8Ints * index);
-            if (last_odd <= pos0 + t) continue;
-            float o[HD / 64], mm, ll;
-            pair_key_by_key<T, HD>(a, seq, g, pos0 + t, key0, key1, (const T *)a.q + (size_t)(row0 + t) * a.q_stride + (size_t)hh * HD, mm, ll, o);
-            float *pp = partial_of<HD>(a, max(slot, 0), col);
-            if (slot >= 0 && lane == 0) {
-                pp[0] = mm;
-                pp[1] = ll;
-            }
-#pragma unroll
-            for (int d = 0; d < HD / 64; ++d) {
-                if (slot >= 0) pp[kPartialPad + lane + 64 * d] = o[d];
-                else ((T *)a.out)[(size_t)(row0 + t) * a.out_stride + (size_t)hh * HD + lane + 64 * d] = from_f32<T>(o[d] * inverse(ll));
-            }
         }
     }
 }

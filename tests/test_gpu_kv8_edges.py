@@ -1,4 +1,5 @@
 """Calls on the 8-bit cache at its edges (bounds in kv8_common.py)."""
+import numpy as np
 import pytest
 import torch
 
@@ -38,3 +39,47 @@ def test_a_value_that_is_not_a_number_in_the_prefix_changes_its_dim_alone(seg, d
     assert o.isfinite().all() and w[:, 2:, 21].isnan().all()
     w[:, 2:, 21] = o[:, 2:, 21]
     assert torch.equal(o, w)
+
+
+@pytest.mark.parametrize("seg", [(0, 50, 4), (0, 9000, 3), (0, 40, 90), (0, 4000, 150)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("prefix", [False, True])
+def test_attention_in_place(seg, dtype, prefix):
+    """out may be q itself, also where sums are taken again because a later row's value is not a number."""
+    shape = ops.HeadShape(4, 2, 64, dtype=dtype)
+    _, off, n = seg
+    b = Both(shape, 1, 600, seed=73)
+    b.fill({0: off + n})
+    value_at(b, 0, off + n - 2, 0, 3).fill_(0xff)
+    if prefix:
+        value_at(b, 0, 5, 0, 40).fill_(0x7f)
+    q = tensor(b.rng.normal(size=(n, 256)), dtype)
+    rows, out = b.rows([seg]), torch.empty(n, 256, device="cuda", dtype=shape.torch_dtype)
+    ops.kv8_attend(rows, b.kv, 0, q, out)
+    if not prefix:
+        b.adopt()
+        b.ref.val[1] = np.nan_to_num(b.ref.val[1], nan=0.0)
+        b.check_attend([seg], q, out, some=set(range(n - 2)))
+        assert out.view(n, 4, 64)[n - 2:, :2, 3].isnan().all()
+    ops.kv8_attend(rows, b.kv, 0, q, q)
+    bits = torch.int16 if dtype == "bf16" else torch.int32
+    assert torch.equal(q.view(bits), out.view(bits))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rot", [32, 128])
+def test_append_in_place(dtype, rot):
+    """The rotated queries may take the place of the rows' own."""
+    shape = ops.HeadShape(14, 2, 128, dtype=dtype, rot_dims=rot)
+    segs = [(0, 3, 40), (1, 0, 1), (2, 30, 5)]
+    x = tensor(np.random.default_rng(8).normal(size=(46, 18 * 128)), dtype)
+    outs = []
+    for place in (False, True):
+        b = Both(shape, 3, 4, seed=77)
+        b.fill({0: 3, 2: 30})
+        y = x.clone()
+        q = y[:, :14 * 128] if place else torch.empty(46, 14 * 128, device="cuda", dtype=shape.torch_dtype)
+        ops.kv8_append(b.rows(segs), b.kv, 0, y, q)
+        assert torch.equal(y[:, 14 * 128:], x[:, 14 * 128:])
+        outs.append([q.clone(), b.kv.k.view(torch.uint8).clone(), b.kv.v.view(torch.uint8).clone(), b.kv.k_scale.clone()])
+    assert all(torch.equal(a.nan_to_num(7.0), c.nan_to_num(7.0)) for a, c in zip(*outs))
