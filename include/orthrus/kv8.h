@@ -117,8 +117,8 @@ int orthrus_kv8_read(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer
  * negative or not finite).  q, out: device [rows][stride] of the shape's dtype, n_q head_dim values a
  * row; strides multiples of 8 elements, bases 16-byte aligned (EINVAL); out may be q itself (base and stride), else the
  * two share no element.  Scores, softmax and sums in
- * fp32; bfloat16 rows round the softmax weights to bfloat16 before the product with the values, fp32 rows keep
- * them whole.  Keys of a page outside [0, n_pages) are skipped (ORTHRUS_DEVERR_PAGE); a row
+ * fp32; bfloat16 rows round the softmax weights to bfloat16 before the product with the values and divide by the sum
+ * of the rounded ones, fp32 rows keep them whole.  Keys of a page outside [0, n_pages) are skipped (ORTHRUS_DEVERR_PAGE); a row
  * left without keys is zero.  A row that sees only scores of minus infinity is not a number, as its softmax. */
 int orthrus_kv8_attend(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer, const void *q, int64_t q_stride,
                        float scale, void *out, int64_t out_stride, void *stream);

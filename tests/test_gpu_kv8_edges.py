@@ -83,3 +83,28 @@ def test_append_in_place(dtype, rot):
         assert torch.equal(y[:, 14 * 128:], x[:, 14 * 128:])
         outs.append([q.clone(), b.kv.k.view(torch.uint8).clone(), b.kv.v.view(torch.uint8).clone(), b.kv.k_scale.clone()])
     assert all(torch.equal(a.nan_to_num(7.0), c.nan_to_num(7.0)) for a, c in zip(*outs))
+
+
+@pytest.mark.parametrize("heads", [(16, 2, 64), (16, 1, 128)])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_equal_values_come_out_whole(heads, rows):
+    """Rows whose values are all 1 give 1: the sum that divides is that of the weights as they were multiplied.  The scores
+    of 64 keys are above the others' by less than 2^8, so that their weights may stay above one, and all round alike."""
+    shape = ops.HeadShape(*heads)
+    nq, _, hd = heads
+    b = Both(shape, rows, 40, seed=83)
+    k, v = b.kv.k.view(torch.uint8), b.kv.v.view(torch.uint8)
+    b.kv.k_scale.fill_(1.0)
+    b.kv.v_scale.fill_(1.0)
+    v.fill_(0x38)                                                       # 1
+    q = torch.zeros(rows, nq, hd, device="cuda")
+    q[..., 0] = tensor(b.rng.uniform(3.0, 5.4, size=(rows, nq)))        # times log2(e): below 8
+    plan = b.rows([(s, 575, 1) for s in range(rows)])
+    for first in (256, 512):                                            # (the second or third 64 keys of one wave of four or eight)
+        k.zero_()
+        for s in range(rows):
+            for p in range(first, first + 64, PAGE):
+                k[0, int(b.table[s][p // PAGE]), :, :, 0] = 0x38
+        out = torch.empty(rows, nq * hd, device="cuda", dtype=torch.bfloat16)
+        ops.kv8_attend(plan, b.kv, 0, q.view(rows, nq * hd).bfloat16(), out, scale=1.0)
+        assert (out == 1.0).all(), (first, float(out.float().min()), float(out.float().max()))
