@@ -128,11 +128,11 @@ int orthrus_kv8_attend(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t lay
  * pairs of whole heads).  The models' heads are within the limits of orthrus_rows_create and the rows within those of
  * orthrus_rows_plan; nothing is enqueued where they are not.  A cache has the models' KV heads and head dimension, at
  * least as many layers (EINVAL), and its pools are given also where a model has no layers.  gen_kv may be emb_kv, or
- * equal to it in every field: then all items share one sequence namespace.  Two caches share no pool and no scale
- * (EINVAL).  workspace: 256-byte aligned, at least orthrus_step_kv8_bytes() for this batch's sizes (arguments as those
- * of orthrus_workspace_bytes; a chunk's end counts as a context for max_ctx), cleared once by orthrus_workspace_init;
- * its error word (orthrus_device_error) also gets the operators' bits.  Host sides of calls that share `emb` run one
- * after the other; one step in flight per workspace.  Not for capture into a HIP graph (EUNSUPPORTED). */
+ * equal to it in every field: then all items share one sequence namespace.  Pools and scales, of two caches
+ * or of one, do not overlap (EINVAL).  workspace: 256-byte aligned, at least orthrus_step_kv8_bytes() for this batch's
+ * sizes (arguments as those of orthrus_workspace_bytes; a chunk's end counts as a context for max_ctx), cleared once by
+ * orthrus_workspace_init; its error word (orthrus_device_error) also gets the operators' bits.  Host sides of calls that
+ * share `emb` run one after the other; one step in flight per workspace.  Not for capture into a HIP graph (EUNSUPPORTED). */
 size_t orthrus_step_kv8_bytes(const orthrus_model *emb, const orthrus_model *gen, int32_t max_tokens, int32_t max_chunks,
                               int32_t max_decode, int32_t max_ctx);
 int orthrus_step_kv8(const orthrus_model *emb, const orthrus_model *gen, const orthrus_batch *batch, const orthrus_kv8 *emb_kv,

@@ -1016,11 +1016,17 @@ int orthrus_step_kv8(const orthrus_model *emb, const orthrus_model *gen, const o
         kv[i] = orthrus_kv{k->k_cache, k->v_cache, k->block_table, k->n_pages, k->n_seq, k->max_blocks};
         if (k->n_layers < emb->cfg.n_layers) return ORTHRUS_EINVAL;
     }
-    // one cache or two: pools, scales, tables and sizes are all the same, or no pool or scale is
-    const orthrus_kv8 &e = *emb_kv, &g = *gen_kv;
-    const bool same = e.k_cache == g.k_cache;
-    if (same ? std::memcmp(&e, &g, sizeof e) != 0
-             : e.v_cache == g.v_cache || e.k_scale == g.k_scale || e.v_scale == g.v_scale) return ORTHRUS_EINVAL;
+    // one cache or two: every field is the same, or pools and scales lie apart; so do those of a cache
+    struct { uintptr_t at; size_t bytes; } part[8];
+    const int n_parts = std::memcmp(emb_kv, gen_kv, sizeof *emb_kv) == 0 ? 4 : 8;
+    for (int i = 0; i < n_parts; ++i) {
+        const orthrus_kv8 &k = i < 4 ? *emb_kv : *gen_kv;
+        const void *const at[4] = {k.k_cache, k.v_cache, k.k_scale, k.v_scale};
+        const size_t heads = (size_t)k.n_layers * k.n_pages * emb->cfg.n_kv_heads;
+        part[i] = {(uintptr_t)at[i % 4], heads * (i % 4 < 2 ? kPage8 * emb->cfg.head_dim : sizeof(float))};
+        for (int j = 0; j < i; ++j)
+            if (part[i].at < part[j].at + part[j].bytes && part[j].at < part[i].at + part[i].bytes) return ORTHRUS_EINVAL;
+    }
     try {
         std::lock_guard<std::mutex> lk(const_cast<orthrus_model *>(emb)->kv8_mu);
         return step_impl(emb, gen, batch, &kv[0], &kv[1], acc_sum, acc_w, out_logits, out_emb, workspace, ws_bytes, stream, false, &k8);
