@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2609_25405_amd import _abi_ops as O
 from paper_2609_25405_amd import ops
 from tests.kv8_common import PAGE, Both, tensor
 
@@ -108,3 +109,39 @@ def test_equal_values_come_out_whole(heads, rows):
         out = torch.empty(rows, nq * hd, device="cuda", dtype=torch.bfloat16)
         ops.kv8_attend(plan, b.kv, 0, q.view(rows, nq * hd).bfloat16(), out, scale=1.0)
         assert (out == 1.0).all(), (first, float(out.float().min()), float(out.float().max()))
+
+
+def test_each_call_of_another_plans_replay_changes_nothing():
+    """Append, read-back and attention captured apart: after the workspace got another plan, each leaves pages, scales and
+    outputs as they are and says so."""
+    shape = ops.HeadShape(8, 2, 128)
+    b = Both(shape, 3, 8, seed=89)
+    segs = [(0, 0, 50), (1, 33, 1), (2, 64, 6)]
+    b.fill({s: o for s, o, _ in segs if o})
+    T = 57
+    x, q = tensor(b.rng.normal(size=(T, 1536)), "bf16"), torch.zeros(T, 1024, device="cuda", dtype=torch.bfloat16)
+    out, ko, vo = torch.zeros_like(q), *(torch.zeros(T, 256, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    rows = b.rows(segs)
+    calls = [lambda: ops.kv8_append(rows, b.kv, 0, x, q), lambda: ops.kv8_attend(rows, b.kv, 0, q, out),
+             lambda: ops.kv8_read(rows, b.kv, 0, ko, vo)]
+    graphs = []
+    for c in calls:
+        c()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c()
+        graphs.append(g)
+    for g in graphs:
+        g.replay()
+    assert rows.device_error() == 0
+    rows.plan(b.kv, [(2, 10, 3), (1, 0, 1)])
+    x.neg_()
+    held = [b.kv.k, b.kv.v, b.kv.k_scale, b.kv.v_scale, q, ko, vo, out]
+    for g in graphs:
+        for t in (q, ko, vo, out):
+            t.fill_(3.0)
+        was = [t.contiguous().view(torch.uint8).clone() for t in held]
+        g.replay()
+        assert rows.device_error() == O.ORTHRUS_DEVERR_STALE
+        assert all(torch.equal(t.contiguous().view(torch.uint8), w) for t, w in zip(held, was))
