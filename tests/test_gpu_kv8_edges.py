@@ -3,9 +3,10 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import kv8 as D
 from paper_2609_25405_amd import _abi_ops as O
 from paper_2609_25405_amd import ops
-from tests.kv8_common import PAGE, Both, tensor
+from tests.kv8_common import PAGE, Both, host, tensor
 
 pytestmark = pytest.mark.gpu
 
@@ -145,3 +146,41 @@ def test_each_call_of_another_plans_replay_changes_nothing():
         g.replay()
         assert rows.device_error() == O.ORTHRUS_DEVERR_STALE
         assert all(torch.equal(t.contiguous().view(torch.uint8), w) for t, w in zip(held, was))
+
+
+def test_keys_and_values_past_four_gigabytes():
+    """Pages behind 4 GiB of each pool: keys and values are held there, read back and attended to, and the pages before are
+    as they were."""
+    shape = ops.HeadShape(8, 8, 128)
+    n_pages = 2 ** 32 // (8 * 2048) + 5
+    kv = ops.DeviceKV8(shape, 1, n_pages, 1, 2)
+    kv.set_block_table(np.array([[n_pages - 1, n_pages - 2]]))
+    x = host(tensor(np.random.default_rng(3).normal(size=(20, 24, 128)), "bf16"))
+    rows = ops.RaggedRows(shape, 20, 1, 20)
+    rows.plan(kv, [(0, 0, 20)])
+    q, o, ko, vo = (torch.empty(20, 1024, device="cuda", dtype=torch.bfloat16) for _ in range(4))
+    ops.kv8_append(rows, kv, 0, tensor(x.reshape(20, -1), "bf16"), q)
+    ops.kv8_read(rows, kv, 0, ko, vo)
+    ops.kv8_attend(rows, kv, 0, q, o)
+    assert rows.device_error() == 0
+    freq = 10000.0 ** (-2.0 * np.arange(64) / 128)
+    turned = np.stack([D.turn(x[t, 8:16], t, freq) for t in range(20)])
+    scale = host(kv.k_scale[0, [n_pages - 1] * 16 + [n_pages - 2] * 4])[..., None]
+    length = np.sqrt(np.sum(turned * turned, -1, keepdims=True))
+    k, v = host(ko).reshape(20, 8, 128), host(vo).reshape(20, 8, 128)
+    assert (np.abs(k - turned) <= np.maximum(2.0 ** -4 * np.abs(turned), 2.0 ** -10 * scale) + 2.0 ** -18 * length).all()
+    vs = host(kv.v_scale[0, [n_pages - 1] * 16 + [n_pages - 2] * 4])[..., None]
+    np.testing.assert_array_equal(v, D.e4m3(x[:, 16:] / vs) * vs)
+    qs, got = host(q).reshape(20, 8, 128), host(o).reshape(20, 8, 128)
+    for t in range(20):
+        for h in range(8):
+            s = k[:t + 1, h] @ qs[t, h] * 128 ** -0.5
+            p = np.exp(s - s.max())
+            p /= p.sum()
+            size = float(np.max(np.abs(k[:t + 1, h]) @ np.abs(qs[t, h]))) * 128 ** -0.5
+            want, mag = p @ v[:t + 1, h], p @ np.abs(v[:t + 1, h])
+            tol = mag * (2.0 ** -8 + 2.0 ** -16 + 2 * size * 2.0 ** -19) + np.abs(want) * 2.0 ** -8 + 1e-30
+            assert (np.abs(got[t, h] - want) <= tol).all(), (t, h)
+    for pool in (kv.k, kv.v):
+        c = pool.view(torch.uint8)[0, :n_pages - 2].view(-1)
+        assert not any(c[i:i + 2 ** 30].any() for i in range(0, c.numel(), 2 ** 30))
