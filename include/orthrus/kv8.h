@@ -114,7 +114,7 @@ int orthrus_kv8_read(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t layer
 /* Causal attention of the planned rows over the cache in layer `layer`: the row at position p of its
  * sequence sees positions 0 .. p (its own key and value appended before); query head h reads KV
  * head h / (n_q / n_kv).  out = softmax(scale * q k^T) v; scale 0 means 1 / sqrt(head_dim) (EINVAL if
- * negative or not finite).  q, out: device [rows][stride] of the shape's dtype, n_q head_dim values a
+ * negative, or not finite once multiplied by log2(e)).  q, out: device [rows][stride] of the shape's dtype, n_q head_dim values a
  * row; strides multiples of 8 elements, bases 16-byte aligned (EINVAL); out may be q itself (base and stride), else the
  * two share no element.  Scores, softmax and sums in
  * fp32; bfloat16 rows round the softmax weights to bfloat16 before the product with the values and divide by the sum

@@ -277,7 +277,9 @@ int orthrus_kv8_attend(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t lay
     const int rc = plan_args(r, kv, layer, a.p);
     if (rc) return rc;
     const orthrus_head_shape &s = r->shape;
-    if (!(scale >= 0.f) || !std::isfinite(scale)) return ORTHRUS_EINVAL;
+    if (scale == 0.f) scale = 1.0f / std::sqrt((float)s.head_dim);
+    const float scale2 = 1.4426950408889634f * scale;
+    if (!(scale > 0.f) || !std::isfinite(scale2)) return ORTHRUS_EINVAL;
     if (r->plan.T == 0) return ORTHRUS_OK;
     const int64_t q_dim = (int64_t)s.n_q_heads * s.head_dim;
     if (!rows_ok(q, q_stride, q_dim) || !rows_ok(out, out_stride, q_dim)) return ORTHRUS_EINVAL;
@@ -296,7 +298,7 @@ int orthrus_kv8_attend(const orthrus_rows *r, const orthrus_kv8 *kv, int32_t lay
     a.off_small = r->plan.off_small;
     a.off_tiles = r->plan.off_tiles;
     a.off_merge = r->plan.off_merge;
-    a.scale = 1.4426950408889634f * (scale > 0.f ? scale : 1.0f / std::sqrt((float)s.head_dim));
+    a.scale = scale2;
     a.partials = partials_of(r);
     return launch_attend8(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
 }

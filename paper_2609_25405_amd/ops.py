@@ -249,10 +249,11 @@ def kv8_attend(rows: RaggedRows, kv: DeviceKV8, layer: int, q: torch.Tensor, out
     kv._fits(s)
     dev = _here(q, out)
     kv._on(dev)
-    _need(scale is None or scale > 0, "scale")
+    sc = 0.0 if scale is None else ctypes.c_float(scale).value       # (what rounds to zero is not the usual scale)
+    _need(scale is None or sc > 0, "scale")
     width = s.n_q_heads * s.head_dim
     stride, out_stride = rows._rows_of(q, width, s.torch_dtype, "q"), rows._rows_of(out, width, s.torch_dtype, "out")
-    _check(O.load().orthrus_kv8_attend(rows.handle, kv._ref, layer, q.data_ptr(), stride, scale or 0.0, out.data_ptr(), out_stride,
+    _check(O.load().orthrus_kv8_attend(rows.handle, kv._ref, layer, q.data_ptr(), stride, sc, out.data_ptr(), out_stride,
                                        _stream(stream, dev)), "orthrus_kv8_attend")
 
 

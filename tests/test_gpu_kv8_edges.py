@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from oracle import kv8 as D
+from paper_2609_25405_amd import _abi as A
 from paper_2609_25405_amd import _abi_ops as O
 from paper_2609_25405_amd import ops
 from tests.kv8_common import PAGE, Both, host, tensor
@@ -184,3 +185,20 @@ def test_keys_and_values_past_four_gigabytes():
     for pool in (kv.k, kv.v):
         c = pool.view(torch.uint8)[0, :n_pages - 2].view(-1)
         assert not any(c[i:i + 2 ** 30].any() for i in range(0, c.numel(), 2 ** 30))
+
+
+def test_scales_that_fp32_does_not_hold():
+    """A scale that rounds to zero in fp32 is refused, not taken for the usual one; so is one that overflows on its
+    way to base 2.  The least and the largest that pass are what they say."""
+    shape = ops.HeadShape(4, 2, 64)
+    b = Both(shape, 1, 8, seed=79)
+    b.fill({0: 100})
+    q = tensor(b.rng.normal(size=(1, 256)), "bf16")
+    rows, out = b.rows([(0, 99, 1)]), torch.empty(1, 256, device="cuda", dtype=torch.bfloat16)
+    for scale in (1e-46, 1e-300, 0.0, 2.4e38, 1e39):
+        with pytest.raises(A.OrthrusError, match=r"\(-1\)"):
+            ops.kv8_attend(rows, b.kv, 0, q, out, scale=scale)
+    ops.kv8_attend(rows, b.kv, 0, q, out, scale=1e-30)
+    b.check_attend([(0, 99, 1)], q, out, scale=1e-30)
+    ops.kv8_attend(rows, b.kv, 0, torch.zeros_like(q), out, scale=2.3e38)
+    b.check_attend([(0, 99, 1)], torch.zeros_like(q), out, scale=2.3e38)
