@@ -130,9 +130,9 @@ class DeviceKV8:
 
 
 def _segments(segments):
-    a = np.ascontiguousarray(np.asarray(segments, dtype=np.int64).reshape(-1, 3))
-    _need(bool((np.abs(a) < 2 ** 31).all()), "segment values")
-    return a.astype(np.int32)
+    a = np.asarray(segments)
+    _need(a.size == 0 or a.dtype.kind in "iu" and bool((a >= -2 ** 31).all() and (a < 2 ** 31).all()), "segment values")
+    return np.ascontiguousarray(a.astype(np.int32).reshape(-1, 3))
 
 
 class RaggedRows:

@@ -1,11 +1,18 @@
 """Refusals of the 8-bit cache's calls at their edges, on the CPU."""
 import ctypes
+import re
 
+import numpy as np
+import pytest
 import torch
 
 from paper_2609_25405_amd import _abi as A
 from paper_2609_25405_amd import _abi_ops as O
 from paper_2609_25405_amd import ops
+
+
+def code_of(rc):
+    return pytest.raises(A.OrthrusError, match=re.escape(f"({rc})"))
 
 
 def test_caches_of_a_step_share_no_pool_and_no_scale():
@@ -46,3 +53,22 @@ def test_caches_of_a_step_share_no_pool_and_no_scale():
     a = -(-big.data_ptr() // 16) * 16
     e, g = changed(kv, k_cache=a, v_cache=a + 2 * pool), changed(other, k_cache=a + pool, v_cache=a + 3 * pool)
     assert call(g, e) == A.ORTHRUS_ECAPACITY
+
+
+@pytest.mark.parametrize("segs", [[(-2 ** 63, 0, 1)], [(2 ** 32, 0, 1)], [(0, -2 ** 31 - 1, 1)], [(0.5, 0, 1)],
+                                  np.array([[2 ** 64 - 2 ** 32, 0, 1]], np.uint64)])
+def test_segments_that_are_no_32_bit_integers_are_refused(segs):
+    shape = ops.HeadShape(8, 4, 128)
+    kv, rows = ops.DeviceKV8(shape, 1, 8, 4, 8, device="cpu"), ops.RaggedRows(shape, 64, 4, 128, device="cpu")
+    with code_of(A.ORTHRUS_EINVAL):
+        rows.items(kv, segs)
+
+
+def test_segments_of_any_integer_type():
+    shape = ops.HeadShape(8, 4, 128)
+    kv, rows = ops.DeviceKV8(shape, 1, 8, 4, 8, device="cpu"), ops.RaggedRows(shape, 64, 4, 128, device="cpu")
+    want = rows.items(kv, [(1, 3, 2)])
+    for dt in (np.int32, np.int64, np.uint8, np.uint64):
+        got = rows.items(kv, np.array([[1, 3, 2]], dt))
+        assert got[0] == want[0] and (got[1] == want[1]).all()
+    assert rows.items(kv, [])[0] == [0, 0, 0, 0]
