@@ -199,7 +199,7 @@ class RaggedRows:
         stride, inner = t.stride()
         if inner != 1:
             raise A.OrthrusError(A.ORTHRUS_EINVAL, what + " strides")
-        return stride if n > 1 else max(stride, width)
+        return stride if n > 1 else width          # (one row's stride is nobody's)
 
 
 def _gain(t, hd):

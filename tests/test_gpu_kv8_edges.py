@@ -202,3 +202,16 @@ def test_scales_that_fp32_does_not_hold():
     b.check_attend([(0, 99, 1)], q, out, scale=1e-30)
     ops.kv8_attend(rows, b.kv, 0, torch.zeros_like(q), out, scale=2.3e38)
     b.check_attend([(0, 99, 1)], torch.zeros_like(q), out, scale=2.3e38)
+
+
+def test_one_row_of_any_stride():
+    """The stride of a tensor of one row is nobody's."""
+    shape = ops.HeadShape(4, 2, 64)
+    b = Both(shape, 1, 8, seed=97)
+    b.fill({0: 100})
+    q = tensor(b.rng.normal(size=(1, 256)), "bf16")
+    odd = torch.empty(1 * 259 + 8, device="cuda", dtype=torch.bfloat16).as_strided((1, 256), (259, 1))
+    odd.copy_(q)
+    rows, out = b.rows([(0, 99, 1)]), torch.empty(1, 256, device="cuda", dtype=torch.bfloat16)
+    ops.kv8_attend(rows, b.kv, 0, odd, out)
+    b.check_attend([(0, 99, 1)], q, out)
