@@ -12,7 +12,8 @@
  *   - While a page fills, its scale never shrinks.  Where a token needs a larger one, the codes
  *     that the page already holds are rounded again under it.
  *   - A position at the start of a page forgets what the page held before.
- *   - Elements that are infinite or not a number are stored as not a number.
+ *   - Elements that are infinite or not a number, or that would round to 2^128 (magnitudes from 0x1.fp127 on, which
+ *     count as infinite), are stored as not a number.
  */
 #ifndef ORTHRUS_KV8_H
 #define ORTHRUS_KV8_H

@@ -10,6 +10,7 @@ import math
 import numpy as np
 
 PAGE = 16
+PAST_RANGE = 1.9375 * 2.0 ** 127        # magnitudes from here on would round to 2^128: as infinities, not a number
 
 
 def e4m3(x):
@@ -63,13 +64,14 @@ class Cache:
             for which, x in ((0, k), (1, v)):
                 for h in range(x.shape[1]):
                     new = x[p0 - offset:p1 - offset, h]
+                    new = np.where(np.abs(new) < PAST_RANGE, new, np.nan)
                     fine = new[np.isfinite(new)]
                     s = page_scale(np.abs(fine).max() if fine.size else 0.0)
                     if first > 0 and self.scale[which][page, h] > s:
                         s = self.scale[which][page, h]
                     tile = self.val[which][page, h]
                     tile[:first] = e4m3(tile[:first] / s) * s
-                    tile[first:last] = e4m3(np.where(np.isfinite(new), new, np.nan) / s) * s
+                    tile[first:last] = e4m3(new / s) * s
                     self.scale[which][page, h] = s
 
     def rows(self, table, seq, a, b):

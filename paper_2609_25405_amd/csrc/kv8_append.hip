@@ -37,6 +37,10 @@ template <int LPR> __device__ __forceinline__ float row_max(float v) {
     return v;
 }
 
+// Magnitudes from here on would round to 2^128 (248 * 2^120, half-way between two codes under the largest scale): not a number
+// as infinities are, so that every held value is finite in fp32 and bfloat16.
+constexpr float kPastRange = 0x1.fp127f;
+
 // the least power of two s with amax <= 448 s = 1.75 * 2^8 s, from amax's exponent and mantissa
 __device__ __forceinline__ float scale_of(float amax) {
     const uint32_t b = __float_as_uint(amax);
@@ -243,7 +247,7 @@ __global__ __launch_bounds__(NT) void append8_kernel(Append8 a) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float v = fabsf(x[c][j]);
-                if (v < INFINITY) m = fmaxf(m, v);
+                if (v < kPastRange) m = fmaxf(m, v);
                 else x[c][j] = NAN;
             }
         m = row_max<LPR>(m);

@@ -215,3 +215,22 @@ def test_one_row_of_any_stride():
     rows, out = b.rows([(0, 99, 1)]), torch.empty(1, 256, device="cuda", dtype=torch.bfloat16)
     ops.kv8_attend(rows, b.kv, 0, odd, out)
     b.check_attend([(0, 99, 1)], q, out)
+
+
+def test_magnitudes_at_the_end_of_the_range():
+    """What would round past the largest power of two that fp32 holds is held as not a number, like an infinity; all below
+    keeps a finite value."""
+    shape = ops.HeadShape(1, 1, 64, dtype="f32", rot_dims=0)
+    b = Both(shape, 2, 1, seed=101)
+    x = np.zeros((2, 3, 64))
+    top = 2.0 ** 120
+    x[0, 1:, :6] = [247.9 * top, -247.9 * top, 248 * top, float(np.finfo(np.float32).max), -255 * top, 225 * top]
+    x[1, 1:, :2] = [224 * top, -1.0]
+    x = host(tensor(x))
+    rows = b.rows([(0, 0, 1), (1, 0, 1)])
+    ops.kv8_append(rows, b.kv, 0, tensor(x.reshape(2, -1)), torch.empty(2, 64, device="cuda"))
+    ko, vo = (torch.empty(2, 64, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    ops.kv8_read(rows, b.kv, 0, ko, vo)
+    for t in (host(ko), host(vo)):
+        assert t[0, [0, 1, 5]].tolist() == [240 * top, -240 * top, 224 * top] and np.isnan(t[0, 2:5]).all()
+        assert t[1, 0] == 224 * top and (t[1, 1:] == 0).all()
