@@ -173,8 +173,8 @@ __device__ void pair_key_by_key(const Attend8 &a, int seq, int head, int pos, in
         const uint8_t *kp = a.p.k + at * (kPage8 * HD) + slot * HD, *vp = a.p.v + at * (kPage8 * HD) + (slot / 4) * (4 * HD) + slot % 4;
         float s = 0.f;
 #pragma unroll
-        for (int d = 0; d < N; ++d) s = fmaf(q[d], bf16_lo(codes_bf16<false>(kp[lane + 64 * d], 1.f)), s);
-        s = wave_sum(s) * (a.scale * a.p.ks[at]);
+        for (int d = 0; d < N; ++d) s = fmaf(q[d], bf16_lo(codes_bf16<false>(kp[lane + 64 * d], a.p.ks[at])), s);
+        s = wave_sum(s) * a.scale;
         const float mn = fmaxf(m, s);
         const float alpha = m == -INFINITY ? 0.f : exp2f(m - mn), p = s == -INFINITY ? 0.f : exp2f(s - mn);
         l = l * alpha + p;
@@ -346,7 +346,7 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
             s[p] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < KK; ++k) {
-                const bf16x8 kf = as_bf16x8(word_bf16(kr[p][k / 2][2 * (k % 2)], 1.f), word_bf16(kr[p][k / 2][2 * (k % 2) + 1], 1.f));
+                const bf16x8 kf = as_bf16x8(word_bf16(kr[p][k / 2][2 * (k % 2)], ks[p]), word_bf16(kr[p][k / 2][2 * (k % 2) + 1], ks[p]));
 #pragma unroll
                 for (int n = 0; n < R::NQ; ++n) s[p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[k][n], s[p], 0, 0, 0);
             }
@@ -361,11 +361,10 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
         float mloc = -INFINITY;
 #pragma unroll
         for (int p = 0; p < PG; ++p) {
-            const float f = ks[p] * a.scale;
             const int seen = min(valid[p], pos + 1 - kbase - p * kPage8);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                s[p][r] = 4 * qd + r < seen ? s[p][r] * f : -INFINITY;
+                s[p][r] = 4 * qd + r < seen ? s[p][r] * a.scale : -INFINITY;
                 mloc = fmaxf(mloc, s[p][r]);
             }
             vs[p] = valid[p] > 0 ? vs[p] : 1.f;

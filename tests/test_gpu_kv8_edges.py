@@ -234,3 +234,31 @@ def test_magnitudes_at_the_end_of_the_range():
     for t in (host(ko), host(vo)):
         assert t[0, [0, 1, 5]].tolist() == [240 * top, -240 * top, 224 * top] and np.isnan(t[0, 2:5]).all()
         assert t[1, 0] == 224 * top and (t[1, 1:] == 0).all()
+
+
+@pytest.mark.parametrize("seg", [(0, 200, 1), (0, 200, 3), (0, 2000, 2)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [None, 1e30])
+def test_scores_are_taken_of_values_not_of_codes(seg, dtype, scale):
+    """Queries whose products with a page's codes leave the range of fp32, while those with its keys do not: the row is the
+    value of its largest score."""
+    shape = ops.HeadShape(4, 2, 64, dtype=dtype)
+    _, off, n = seg
+    b = Both(shape, 1, 130, seed=103)
+    b.fill({0: off + n})
+    size = 2.0 ** 120 if scale is None else 2.0 ** 10
+    down = 2.0 ** -40 if scale is None else 1.0
+    b.kv.k_scale.mul_(down)
+    b.adopt()
+    q = torch.zeros(n, 4, 64, device="cuda", dtype=shape.torch_dtype)
+    q[:, :, 7] = size
+    out = torch.empty(n, 256, device="cuda", dtype=shape.torch_dtype)
+    ops.kv8_attend(b.rows([seg]), b.kv, 0, q.view(n, 256), out, scale=scale)
+    k, v = b.ref.rows(b.table, 0, 0, off + n)
+    for t in range(n):
+        for h in range(4):
+            s = k[:off + t + 1, h // 2, 7]
+            most = s == s.max()
+            want = v[:off + t + 1, h // 2][most].mean(0)
+            tol = 2.0 ** (-7 if dtype == "bf16" else -22) * np.abs(v[:off + t + 1, h // 2][most]).mean(0)
+            assert (np.abs(host(out[t].view(4, 64)[h]) - want) <= tol).all(), (t, h)
