@@ -497,6 +497,8 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
 
 // ------------------------------------------------------------------ tiles of longer segments
 constexpr int kWindow = 256;      // pages
+// (a weight's exponent is then off by up to 2^-4, less than the fp32 score it comes from)
+constexpr float kLargeScore = 0x1p20f;
 
 template <int HD> struct Stage8 {
     static constexpr int KEYS = 64, KRB = HD * 2, KCH = KRB / 16;
@@ -637,7 +639,8 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
     auto v_frag = [&](int buf, int i) { return *(const bf16x8 *)(smem + buf * St::BYTES + (i / DB) * St::VPAGE + (i % DB) * 1024 + v_at); };
     // masks block b's scores, whose maximum is mx if none is masked, and raises the running maximum; bit p of `bad`:
     // page p is bad (its keys are masked, their codes were zeroed)
-    float neg = 0.f;               // minus the maximum, or zero
+    float neg = 0.f;               // minus the maximum times the scale, or zero
+    float neg_now = 0.f;           // what the step at hand adds
     auto raise = [&](int b, uint32_t bad, f32x16 (&s)[2], float mx) {
         const int base = key0 + b * St::KEYS;
         if (base + St::KEYS > first_pos || base + St::KEYS > key1 || bad) {
@@ -652,17 +655,28 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
                 }
         }
         const float2 p = partner32(mx);
-        const float mloc = fmaxf(p.x, p.y) * a.scale;
-        // the maximum follows in jumps of more than 2^8, so that the sums are rarely rescaled
-        if (__ballot(mloc > m + 8.f) != 0) {
-            const float mn = fmaxf(m, mloc), alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        const float mloc = fmaxf(p.x, p.y);
+        // the maximum (of scores before their scale) follows in jumps of more than 2^8, so that the sums are rarely rescaled
+        if (__ballot((mloc - m) * a.scale > 8.f) != 0) {
+            const float mn = fmaxf(m, mloc), alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.scale);
             l *= alpha;
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[d][e] *= alpha;
             m = mn;
-            neg = m == -INFINITY ? 0.f : -m;
+            neg = m == -INFINITY ? 0.f : -m * a.scale;
+        }
+        // What rounding `neg` left out stays in the fused exponents: nothing beside the scores' own errors, but weights out of
+        // range where the exponents are large.  Then the difference is taken first.
+        neg_now = neg;
+        if (__ballot(fabsf(neg) > kLargeScore) != 0) {
+            const float sub = m == -INFINITY ? 0.f : m;
+            neg_now = 0.f;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[j][e] -= sub;
         }
     };
     auto bad_pages = [&](int b) {
@@ -740,7 +754,7 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
             ring[i % AHEAD] = i + AHEAD < NA ? k_frag(P ^ 1, i + AHEAD) : v_frag(P, i + AHEAD - NA);
 #pragma unroll
             for (int e = EA * i; e < EA * (i + 1); ++e) {
-                s[e / 16][e % 16] = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], a.scale, neg));
+                s[e / 16][e % 16] = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], a.scale, neg_now));
                 if (R::NP > 1) l += s[e / 16][e % 16];
             }
             if ((EA * (i + 1)) % 8 == 0) {
@@ -857,7 +871,7 @@ template <typename T, int HD> __device__ __forceinline__ void tile_item(const At
         if (slot >= 0) {
             float *pp = partial_of<HD>(a, slot, c);
             if (half == 0) {
-                pp[0] = m;
+                pp[0] = m * a.scale;
                 pp[1] = l;
             }
 #pragma unroll

@@ -262,3 +262,33 @@ def test_scores_are_taken_of_values_not_of_codes(seg, dtype, scale):
             want = v[:off + t + 1, h // 2][most].mean(0)
             tol = 2.0 ** (-7 if dtype == "bf16" else -22) * np.abs(v[:off + t + 1, h // 2][most]).mean(0)
             assert (np.abs(host(out[t].view(4, 64)[h]) - want) <= tol).all(), (t, h)
+
+
+@pytest.mark.parametrize("seg", [(0, 150, 51), (0, 0, 130), (0, 9000, 40), (0, 500, 3), (0, 1500, 1)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [2.0 ** 18, 2.0 ** 24, 2.0 ** 40, 2.0 ** 100])
+def test_scores_of_any_size(seg, dtype, size):
+    """The row of scores far apart is the value of the largest, whatever their size; several heads, of which one has ordinary
+    scores."""
+    shape = ops.HeadShape(4, 2, 64, dtype=dtype)
+    _, off, n = seg
+    b = Both(shape, 1, 600, seed=107)
+    b.fill({0: off + n})
+    q = torch.zeros(n, 4, 64, device="cuda", dtype=shape.torch_dtype)
+    q[:, :, 7] = size
+    q[:, 1, 7] = -size
+    q[:, 3] = tensor(b.rng.normal(size=(n, 64)))
+    out = torch.empty(n, 256, device="cuda", dtype=shape.torch_dtype)
+    ops.kv8_attend(b.rows([seg]), b.kv, 0, q.view(n, 256), out)
+    b.check_attend([seg], q, out, some=set(range(0, n, 13)))           # (bounds of the ordinary head)
+    k, v = b.ref.rows(b.table, 0, 0, off + n)
+    got = host(out.view(n, 4, 64))
+    for t in range(0, n, 13):
+        for h in range(3):
+            s = k[:off + t + 1, h // 2, 7] * (-1 if h == 1 else 1)
+            gap = s.max() - s
+            if gap[gap > 0].size and gap[gap > 0].min() * size / 8 < 2000:
+                continue
+            most = gap == 0
+            want, mag = v[:off + t + 1, h // 2][most].mean(0), np.abs(v[:off + t + 1, h // 2][most]).mean(0)
+            assert (np.abs(got[t, h] - want) <= 2.0 ** (-7 if dtype == "bf16" else -20) * mag).all(), (t, h)
