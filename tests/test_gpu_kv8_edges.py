@@ -292,3 +292,34 @@ def test_scores_of_any_size(seg, dtype, size):
             most = gap == 0
             want, mag = v[:off + t + 1, h // 2][most].mean(0), np.abs(v[:off + t + 1, h // 2][most]).mean(0)
             assert (np.abs(got[t, h] - want) <= 2.0 ** (-7 if dtype == "bf16" else -20) * mag).all(), (t, h)
+
+
+@pytest.mark.parametrize("seg", [(0, 1000, 90), (0, 37, 130), (0, 30, 3), (0, 2111, 2), (0, 9001, 40)])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (14, 2, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [False, True])
+def test_rows_before_a_value_that_is_not_a_number(seg, heads, dtype, bad):
+    """Their sums are taken again without it: in tiles and small items, over whole and partial steps, pieces, and past a bad
+    page."""
+    shape = ops.HeadShape(*heads, dtype=dtype)
+    nq, nkv, hd = heads
+    _, off, n = seg
+    b = Both(shape, 1, 600, seed=109)
+    b.fill({0: off + n})
+    last = off + n - 1
+    for d in range(hd):
+        value_at(b, 0, last, d % nkv, d).fill_(0x7f if d % 3 else 0xff)
+    skip = ()
+    if bad:
+        b.table[0][1], skip = -1, (-1,)
+        b.kv.set_block_table(b.table)
+    b.adopt()
+    b.ref.val[1] = np.nan_to_num(b.ref.val[1], nan=0.0)
+    q = tensor(b.rng.normal(size=(n, nq * hd)) * 2, dtype)
+    rows, out = b.rows([seg]), torch.empty(n, nq * hd, device="cuda", dtype=shape.torch_dtype)
+    ops.kv8_attend(rows, b.kv, 0, q, out)
+    assert rows.device_error() == (A.ORTHRUS_DEVERR_PAGE if bad else 0)
+    b.check_attend([seg], q, out, some=set(range(0, n - 1, 7)) | {max(n - 2, 0)}, skip=skip)
+    got = out[n - 1].view(nkv, nq // nkv, hd).isnan()
+    for g in range(nkv):
+        assert got[g, :, g::nkv].all() and not got[g, :, 1 - g::nkv].any()
