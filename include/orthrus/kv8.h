@@ -11,7 +11,8 @@
  *     max |x| <= 448 * 2^e over the finite elements of the page's tokens so far.
  *   - While a page fills, its scale never shrinks.  Where a token needs a larger one, the codes
  *     that the page already holds are rounded again under it.
- *   - A position at the start of a page forgets what the page held before.
+ *   - A position at the start of a page forgets what the page held before.  Appending before positions that the page
+ *     holds gives those up: their codes stay, but not their scale.
  *   - Elements that are infinite or not a number, or that would round to 2^128 (magnitudes from 0x1.fp127 on, which
  *     count as infinite), are stored as not a number.
  */

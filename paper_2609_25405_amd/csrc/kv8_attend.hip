@@ -16,7 +16,7 @@
 // Tiles (128 pairs of a longer segment): four waves of 32 pairs; 64-key blocks are turned into bf16 once
 // per workgroup on their way into LDS (two buffers, the next block's codes in flight in registers).  Bound by the matrix pipe with
 // the softmax's vector work beside it: 2 x 512 rows after 7680 keys, 32 query heads over 8, 134 GFLOP in 142 us and the
-// merge of their pieces in 11.
+// merge of their pieces in 11.  fp32 rows have three times the products: 64 rows of 1024 to 4096 keys 81 us, those chunks 388.
 //
 // Long key ranges come as pieces that leave (max, sum, unnormalised output) to a merge launch.  (Joining
 // them in the workgroup that arrives last was five times slower: its device-scope release and acquire write back and
@@ -903,8 +903,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) void attend8_small
 template <int HD> constexpr int kTileLds = 2 * Stage8<HD>::BYTES + kWindow * 12;
 
 // Tiles, and behind them the small items of a batch that has both: one launch after another left the chip to the tail
-// of the first (2 x 512 rows after 7680 keys beside 14 rows of 2048: 163 us apart, 153 jointly; 64 rows after 512 keys
-// beside 64 rows of 2048: 68 and 53; 256 rows of 4096 beside 4 fresh prompts of 512: 399 and 400).
+// of the first (2 x 512 rows after 7680 keys beside 14 rows of 2048: 163 us apart, 152 jointly; 64 rows after 512 keys
+// beside 64 rows of 2048: 68 and 53; 256 rows of 4096 beside 4 fresh prompts of 512: 399 and 400).  Jointly a small item has four
+// waves, also where apart it would have eight and the chip is mostly idle (64 fresh rows beside one of 4000 keys 22.4 us apart,
+// 15.3 jointly; 2 x 100 beside 4 of 900 19.9 and 10.8; 12 small fp32 segments 24.5 and 16.3).
 template <typename T, int HD, bool SMALL>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend8_tile_kernel(Attend8 a) {
     __shared__ __attribute__((aligned(16))) char smem[kTileLds<HD>];

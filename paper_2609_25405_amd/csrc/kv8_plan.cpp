@@ -14,11 +14,11 @@ namespace orthrus {
 namespace {
 // Key ranges.  An item walks its keys in steps, so one long range can outlast the launch while CUs are
 // idle: ranges longer than their share of the launch's workgroup slots are cut into pieces of about that share, on
-// multiples of kCut keys.  A piece costs its partial sums' way through memory and, with the others, a merge launch of
-// about 5 us, so it has a least length.
+// multiples of kCut keys.  A piece costs its partial sums' way through memory and, with the others, a merge launch (5 us for
+// 64 rows, 11 for two chunks of 512), so it has a least length.
 constexpr int kCut = 64;
-// Small items run three workgroups of four waves a CU (64 rows of 2560 keys over 8 KV heads 60 us; cut for 1024 slots
-// 66, for 512 60; contexts of 1024 to 4096 61, 64 and 67 us).
+// Small items run three workgroups of four waves a CU (8 KV heads, cut for 512, 768 and 1024 slots: 64 rows of 2560 keys
+// 62.8, 62.8 and 68.8 us, of 1024 to 4096 71.2, 67.0 and 69.4, 100 rows of 3000 123 each, 40 of 6000 100.9, 100.9 and 97.8).
 constexpr int kSlotsSmall = 768, kMinPieceSmall = 1024;
 // Few of them run with eight waves each, cut for fewer workgroups (one row of 4000 keys over 8 KV heads 12.5 us in
 // pieces of at least 512 keys, 14.5 of 1024; 16 rows of 2000 17.6 us in 192 slots, 18.8 in 256, 21.9 in 384).
@@ -27,7 +27,10 @@ constexpr int kWideItems = 256, kSlotsWide = 192, kMinPieceWide = 512;
 // and 10.2; 4 rows of 1400 13.6 and 11.6).
 constexpr int kMostWhole = 1024;
 // Tiles run two workgroups a CU; items i and kCus + i of a launch share one, so the second round comes shortest first
-// (4 fresh prompts of 400 to 623 tokens 26.9 -> 26.5 us).
+// (4 fresh prompts of 400 to 623 tokens 26.9 -> 26.5 us).  The least piece (32 query heads over 8, pieces from 256, 512, 1024
+// and 2048 keys on): 64 rows after 900 keys 18, 22, 26 and 26 us, 128 after 4000 34, 30, 33 and 49, 512 after 2000 40, 40, 41
+// and 53, four prompts of 512 33, 22, 23 and 23, 2 x 512 after 7680 152 each; fp32, 2 x 256 after 1000, 59, 49, 64 and 64.  512
+// is the better one for a chunk or two alone.
 constexpr int kCus = 256, kSlotsTile = 2 * kCus, kMinPieceTile = 1024;
 
 int64_t piece_keys(int64_t total, int slots, int least) {
