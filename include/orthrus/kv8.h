@@ -13,7 +13,7 @@
  *     that the page already holds are rounded again under it.
  *   - A position at the start of a page forgets what the page held before.  Appending before positions that the page
  *     holds gives those up: their codes stay, but not their scale.
- *   - Elements that are infinite or not a number, or that would round to 2^128 (magnitudes from 0x1.fp127 on, which
+ *   - Elements that are infinite or not a number, or that would round to 2^128 (magnitudes from 1.9375 * 2^127 on, which
  *     count as infinite), are stored as not a number.
  */
 #ifndef ORTHRUS_KV8_H

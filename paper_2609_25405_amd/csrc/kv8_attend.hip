@@ -497,7 +497,8 @@ template <typename T, int HD, int NW> __device__ __forceinline__ void small_item
 
 // ------------------------------------------------------------------ tiles of longer segments
 constexpr int kWindow = 256;      // pages
-// (a weight's exponent is then off by up to 2^-4, less than the fp32 score it comes from)
+// exponents from which a tile takes the difference first (up to there the rounding of the maximum times the scale leaves at
+// most 2^-4 in a weight's exponent, no more than the fp32 score's own error)
 constexpr float kLargeScore = 0x1p20f;
 
 template <int HD> struct Stage8 {

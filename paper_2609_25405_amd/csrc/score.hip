@@ -1,9 +1,9 @@
 // Scores of tokens under logits: log probability, entropy, rank and the largest entries of each row.
 //
 // A row is read once: a workgroup holds its slice of up to kSliceMost entries in registers; each thread sums its own under the
-// largest of them so far, eight at a time as they arrive, and the sums meet under the slice's (1999 rows of 131072 entries 169 us, 6.2 TB/s; 256 rows
-// of 32000 with 20 alternatives 11.6 us).  Longer rows are several slices, joined by a
-// second launch of one wave a row.
+// largest of them so far, eight at a time as they arrive, and the sums meet under the slice's (1999 rows of 131072 entries
+// 169 us, 6.2 TB/s; 256 rows of 32000 with 20 alternatives 11.6 us).  Longer rows are several slices, joined by a second
+// launch of one wave a row.
 //
 // Order.  An entry's key is its value as an order-preserving integer (NaN above everything, -0 equal to +0) over the
 // complement of its index, so all keys differ and equal values rank by index.

@@ -87,7 +87,8 @@ class DeviceKV8:
 
     @classmethod
     def from_pools(cls, shape: HeadShape, k, v, k_scale, v_scale, block_table) -> "DeviceKV8":
-        """A cache over tensors that the caller holds (not copied)."""
+        """A cache over tensors that the caller holds (not copied).  Scales are powers of two: of another only the
+        exponent would count."""
         kv = cls.__new__(cls)
         kv._set(shape, k, v, k_scale, v_scale, block_table)
         return kv
@@ -212,7 +213,8 @@ def _gain(t, hd):
 def kv8_append(rows: RaggedRows, kv: DeviceKV8, layer: int, qkv: torch.Tensor, q_out: torch.Tensor,
                q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
     """Head norms, rotation and append of the planned rows of qkv [rows][(n_q + 2 n_kv) hd] (the
-    shape's dtype, or fp32); the rotated queries go to q_out [rows][n_q hd]."""
+    shape's dtype, or fp32); the rotated queries go to q_out [rows][n_q hd], which may be the query columns of qkv
+    in the same dtype."""
     s = rows.shape
     kv._fits(s)
     dev = _here(qkv, q_out, q_gain, k_gain)
@@ -243,8 +245,8 @@ def kv8_read(rows: RaggedRows, kv: DeviceKV8, layer: int, k_out: torch.Tensor, v
 
 def kv8_attend(rows: RaggedRows, kv: DeviceKV8, layer: int, q: torch.Tensor, out: torch.Tensor, scale: Optional[float] = None,
                stream: Optional[int] = None) -> None:
-    """Causal attention of the planned rows: q, out [rows][n_q hd] of the shape's dtype; ``scale``
-    None: 1 / sqrt(hd)."""
+    """Causal attention of the planned rows: q, out [rows][n_q hd] of the shape's dtype (out may be
+    q); ``scale`` None: 1 / sqrt(hd)."""
     s = rows.shape
     kv._fits(s)
     dev = _here(q, out)
