@@ -88,8 +88,8 @@ size_t orthrus_linear_bytes(const orthrus_linear_weights *w, int32_t rows);
 
 /* y[r] = act(x[r] W^T + bias) + residual[r], or for gated weights act(x W^T + bias) * (x U^T + bias_u) +
  * residual; w->groups is 1.  x: rows of k elements of the weights' type; 16-byte aligned, row stride a multiple of 16
- * bytes; for MX8 scales 4-byte aligned, scale_stride a multiple of 4 (the words that hold a row's last
- * elements are read whole).  y: rows of n elements, F32, BF16 or MX8, any stride and alignment to an element.  epilogue NULL:
+ * bytes; for MX8 scales 4-byte aligned, scale_stride a multiple of 4 (the 16 bytes, of scales the 4, that hold a row's last
+ * elements are read whole, what lies between rows may be read, and nothing outside of these is).  y: rows of n elements, F32, BF16 or MX8, any stride and alignment to an element.  epilogue NULL:
  * none.  Sums in fp32, in an order that depends on the sizes alone; bf16 products are exact.  The matrix cores add 8-bit
  * products eight neighbours at a time, without the bits below 2^-13 of the power of two of the largest of the eight.
  * workspace: 16-byte aligned, one call in flight; calls may be captured into graphs.  EINVAL: null pointers, sizes, strides or

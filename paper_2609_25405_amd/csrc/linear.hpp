@@ -64,6 +64,31 @@ struct Product {
     Epilogue e;
 };
 
+// Where the copies of linear_tile.hip read, in bytes from the tile's first row of x (first tile of the weights): the part of the address
+// that a lane holds, which is compared with the buffer's length, and the part that all lanes share, on whose part in that comparison
+// nothing here relies.  A tile's rows may be fewer than its copies', and a step's bytes more than what is left of a row: of x all of the
+// address is the lane's.  The weights' tiles are whole, and a tile that is not there is told by the lane's part.
+struct CopyAt {
+    unsigned lane, shared;
+};
+// 16 bytes of a row of x, of a step of K; the buffer ends with the last row's last 16 bytes
+constexpr CopyAt x_copy(int row, int chunk, int step, unsigned stride) {
+    return CopyAt{row * stride + step * kStepBytes + chunk * 16, 0};
+}
+constexpr int64_t x_room(int rows, int64_t stride, int k_bytes) { return (rows - 1) * stride + (k_bytes + 15) / 16 * 16; }
+// a word of scales of a row of x; `row` is 16 rows' first, `lane_row` the one of them, `words` that of four steps' first
+constexpr CopyAt x_scale_copy(int row, int lane_row, int words, int lane_word, unsigned stride) {
+    return CopyAt{(row + lane_row) * stride + (words + lane_word) * 4, 0};
+}
+constexpr int64_t x_scale_room(int rows, int64_t stride, int k_blocks) { return (rows - 1) * stride + (k_blocks + 3) / 4 * 4; }
+// 16 bytes of a half of a weight tile's step, and a lane's word of scales of a quad of tiles
+constexpr CopyAt w_copy(int half, int lane, int step, unsigned tile_bytes) {
+    return CopyAt{half / 2 * tile_bytes + half % 2 * 1024 + lane * 16, (unsigned)step * kTileBytes};
+}
+constexpr CopyAt w_scale_copy(int quad, int lane, int step, unsigned steps) {
+    return CopyAt{quad * steps * 256 + lane * 4, (unsigned)step * 256};
+}
+
 // the cover of a product by workgroups
 struct ProductPlan {
     int shape;          // of linear_tile.hip, or -1: few rows (linear_few.hip)

@@ -72,50 +72,46 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void tile_kernel(Product p) {
     // the tile's rows of x and of the weights as buffers: what lies behind the last row reads as zero
     const int valid = min(BM, u.row_end - u.row0), b_valid = min(BN / 16, p.shape.tiles - tile0);
     const char *const wg = p.w + u.group * p.group_bytes;
-    const __amdgpu_buffer_rsrc_t ra = buffer_of(p.x + (int64_t)u.row0 * p.x_stride, (valid - 1) * p.x_stride + (p.k_bytes + 15) / 16 * 16);
+    const __amdgpu_buffer_rsrc_t ra = buffer_of(p.x + (int64_t)u.row0 * p.x_stride, x_room(valid, p.x_stride, p.k_bytes));
     const __amdgpu_buffer_rsrc_t rb = buffer_of(wg + tile0 * p.shape.tile_bytes, b_valid * p.shape.tile_bytes);
     const __amdgpu_buffer_rsrc_t rsa = buffer_of(MX ? (const char *)p.x_scale + (int64_t)u.row0 * p.x_scale_stride : nullptr,
-                                                 MX ? (valid - 1) * p.x_scale_stride + (p.k_blocks + 3) / 4 * 4 : 0);
+                                                 MX ? x_scale_room(valid, p.x_scale_stride, p.k_blocks) : 0);
     const __amdgpu_buffer_rsrc_t rsb = buffer_of(MX ? wg + p.shape.scale_at + (size_t)(tile0 / 4) * steps * 256 : nullptr,
                                                  MX ? (size_t)((b_valid + 3) / 4) * steps * 256 : 0);
     // LDS row r of x holds 16-byte chunk c at chunk c ^ key(r), so that the 16 lanes of a pass of a fragment read (16
     // rows, the same chunk) hit distinct banks; a copy's lane l writes row r0 + l / 8 at chunk l % 8 and fetches
     // what is stored there.  Weights lie as they are packed: 1024 bytes a half of a tile of 16.
     auto key_of = [](int row) { return (row / 2) % 8; };
-    unsigned avo[A_I], bvo[B_I];
-#pragma unroll
-    for (int i = 0; i < A_I; ++i) {
+    auto x_at = [&](int i, int step) {
         const int row = 8 * (W * i + wave) + lane / 8;
-        avo[i] = row * (unsigned)p.x_stride + ((lane % 8) ^ key_of(row)) * 16;
-    }
-#pragma unroll
-    for (int i = 0; i < B_I; ++i) {
-        const int half = W * i + wave;
-        bvo[i] = (half / 2) * (unsigned)p.shape.tile_bytes + half % 2 * 1024 + lane * 16;
-    }
+        return x_copy(row, (lane % 8) ^ key_of(row), step, (unsigned)p.x_stride);
+    };
+    auto w_at = [&](int i, int step) { return w_copy(W * i + wave, lane, step, (unsigned)p.shape.tile_bytes); };
     const int sb_i = wave % SB_N;
     // The scales of x: a copy fetches the words of four steps of 16 rows, since a word a row would cost as many requests as the
     // codes do (at 2048 x 4096 x 14336 147 us against 125 without any).  Step t issues quarter (t + AHEAD) % 4 of the rows' words of
     // the four steps from 4 ((t + AHEAD) / 4) on: the last quarter R steps before the first of them.
     constexpr int QUARTER = BM / 16 / 4, AHEAD = R + 3, SETS = scale_sets(R);       // sixteens of rows in a quarter
     static_assert(R <= 6, "a set is read before it is filled again");
-    const unsigned savo = MX ? (lane / 4) * (unsigned)p.x_scale_stride + lane % 4 * 4 : 0;
     auto copy_sa = [&](int i, int m, int q) {
         const int at = m * QUARTER + (W * i + wave) % QUARTER;          // (waves without rows of their own repeat another's)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsa, (lds_void *)(smem + SA_AT + ((q & (SETS - 1)) * (BM / 16) + at) * 256), 4, savo,
-                                                 at * 16 * (int)p.x_scale_stride + (kt0 + 4 * q) * 4, 0, 0);
+        const CopyAt c = x_scale_copy(at * 16, lane / 4, kt0 + 4 * q, lane % 4, (unsigned)p.x_scale_stride);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsa, (lds_void *)(smem + SA_AT + ((q & (SETS - 1)) * (BM / 16) + at) * 256), 4, c.lane,
+                                                 c.shared, 0, 0);
     };
-    const unsigned sbvo = MX ? sb_i * (unsigned)steps * 256 + lane * 4 : 0;
     // copy i of a step: x, then weights, then the scales (which waves fetch more than once where there are few)
     auto copy = [&](auto i_c, int kt, char *st) {
         constexpr int i = decltype(i_c)::value;
-        if constexpr (i < A_I)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void *)(st + (W * i + wave) * 1024), 16, avo[i], (kt0 + kt) * kStepBytes, 0, 0);
-        else if constexpr (i < A_I + B_I)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void *)(st + B_AT + (W * (i - A_I) + wave) * 1024), 16, bvo[i - A_I],
-                                                     (kt0 + kt) * kTileBytes, 0, 0);
-        else
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsb, (lds_void *)(st + SB_AT + sb_i * 256), 4, sbvo, (kt0 + kt) * 256, 0, 0);
+        if constexpr (i < A_I) {
+            const CopyAt c = x_at(i, kt0 + kt);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void *)(st + (W * i + wave) * 1024), 16, c.lane, c.shared, 0, 0);
+        } else if constexpr (i < A_I + B_I) {
+            const CopyAt c = w_at(i - A_I, kt0 + kt);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void *)(st + B_AT + (W * (i - A_I) + wave) * 1024), 16, c.lane, c.shared, 0, 0);
+        } else {
+            const CopyAt c = w_scale_copy(sb_i, lane, kt0 + kt, (unsigned)steps);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsb, (lds_void *)(st + SB_AT + sb_i * 256), 4, c.lane, c.shared, 0, 0);
+        }
     };
 
     f32x16 acc[FM][FN];
