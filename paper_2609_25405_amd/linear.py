@@ -15,7 +15,7 @@ import torch
 
 from . import _abi as A
 from . import _abi_linear as L
-from .ops import _check, _need, _ptr, _stream
+from .ops import _check, _need, _room, _stream
 
 BLOCK = L.ORTHRUS_MX8_BLOCK
 _pack = struct.Struct("=QQqqi4x").pack          # an orthrus_matrix (a ctypes struct takes three times as long to make)
@@ -199,6 +199,7 @@ def _product(w, x, offsets, y, bias, act, residual, workspace, stream):
     rows = shape[0]
     if shape[1] != w.k:
         raise A.OrthrusError(A.ORTHRUS_EINVAL, "x width")
+    ws, ws_bytes = _room(workspace)
     dev = x.get_device()
     _here(dev, w, offsets, bias, workspace)
     out = (rows, w.n)
@@ -215,7 +216,6 @@ def _product(w, x, offsets, y, bias, act, residual, workspace, stream):
         if residual is not None:
             e.residual = L.orthrus_matrix.from_buffer_copy(_ref(residual, out, dev, "residual"))
         e = byref(e)
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
     lib, stream = _lib or _load(), _raw_stream(dev) if stream is None else stream
     at, to = _ref(x, shape, dev, "x"), _ref(y, out, dev, "y")
     if offsets is None:

@@ -53,6 +53,14 @@ def _stream(stream, dev=None):
     return current_stream() if dev is None else torch._C._cuda_getCurrentRawStream(dev)
 
 
+def _room(workspace: Optional[torch.Tensor]):
+    """Address and bytes of a workspace, whose elements lie side by side (an expanded tensor's would be fewer than it counts)."""
+    if workspace is None:
+        return None, 0
+    _need(workspace.is_contiguous(), "workspace")
+    return workspace.data_ptr(), workspace.nbytes
+
+
 class HeadShape:
     """Heads of a layer and how they turn (orthrus_head_shape).  ``rot_dims`` None: the whole head;
     ``rope_freq``: angle per position of each pair (rot_dims / 2 float64), None: from ``rope_base``."""
@@ -310,8 +318,8 @@ def logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, logpro
                          (entropy, torch.float32, (R,)), (top_ids, torch.int32, (R, n)), (top_logprobs, torch.float32, (R, n))):
         if t is not None and not (t.dtype == dt and t.shape == shape and t.is_contiguous()):
             raise A.OrthrusError(A.ORTHRUS_EINVAL, "score tensors")
+    ws, ws_bytes = _room(workspace)
     dev = _here(logits, tokens, logprob, entropy, rank, top_ids, top_logprobs, workspace)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     stride = logits.stride(0) if R > 1 else max(V, logits.stride(0))
     _check(O.load().orthrus_logprobs(_ptr(logits), stride, R, V, _ptr(tokens), n, _ptr(logprob), _ptr(entropy), _ptr(rank),
-                                     _ptr(top_ids), _ptr(top_logprobs), _ptr(workspace), ws_bytes, _stream(stream, dev)), "orthrus_logprobs")
+                                     _ptr(top_ids), _ptr(top_logprobs), ws, ws_bytes, _stream(stream, dev)), "orthrus_logprobs")
