@@ -36,7 +36,7 @@ class Mx8:
         _need(codes.dtype == torch.float8_e4m3fn and codes.dim() == 2, "codes")
         rows, width = codes.shape
         _need(scales.dtype == torch.float8_e8m0fnu and scales.shape == (rows, -(-width // BLOCK)), "scales")
-        self.codes, self.scales, self.shape = codes, scales, codes.shape
+        self._tensors, self._shape = (codes, scales), codes.shape
         self._device = codes.get_device()
         _need(scales.get_device() == self._device, "codes and scales on one device")
         self._ref = _pack(codes.data_ptr(), scales.data_ptr(), _row_stride(codes, "codes"), _row_stride(scales, "scales"), L.ORTHRUS_MX8)
@@ -55,6 +55,11 @@ class Mx8:
         m.codes.view(torch.uint8).copy_(codes.view(torch.uint8))
         m.scales.view(torch.uint8).copy_(scales.view(torch.uint8))
         return m
+
+    # the tensors stay the ones the rows were made of
+    codes = property(lambda self: self._tensors[0])
+    scales = property(lambda self: self._tensors[1])
+    shape = property(lambda self: self._shape)
 
     def get_device(self) -> int:
         return self._device
@@ -177,12 +182,19 @@ class LinearWeights:
         nbytes = int(L.load().orthrus_linear_packed_bytes(byref(self._struct)))
         if nbytes == 0:
             raise A.OrthrusError(A.ORTHRUS_EUNSUPPORTED if dtype == A.ORTHRUS_F32 else A.ORTHRUS_EINVAL, "orthrus_linear_packed_bytes")
-        self.packed = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{dev}")
-        self._struct.packed = self.packed.data_ptr()
+        self._packed = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{dev}")
+        self._struct.packed = self._packed.data_ptr()
         self._ref = byref(self._struct)
-        self.n, self.k, self.groups, self.gated = all_rows // groups, k, groups, up is not None
+        self._sizes = (all_rows // groups, k, groups, up is not None)
         self._device = dev
         _check(L.load().orthrus_linear_pack(self._ref, m, second, _stream(stream, dev)), "orthrus_linear_pack")
+
+    # bytes and sizes stay the ones that were packed
+    packed = property(lambda self: self._packed)
+    n = property(lambda self: self._sizes[0])
+    k = property(lambda self: self._sizes[1])
+    groups = property(lambda self: self._sizes[2])
+    gated = property(lambda self: self._sizes[3])
 
     def get_device(self) -> int:
         return self._device
@@ -197,12 +209,13 @@ def linear_workspace(w: LinearWeights, rows: int, device="cuda") -> Optional[tor
 def _product(w, x, offsets, y, bias, act, residual, workspace, stream):
     shape = _shape2(x, "x")
     rows = shape[0]
-    if shape[1] != w.k:
+    n, k, groups, gated = w._sizes
+    if shape[1] != k:
         raise A.OrthrusError(A.ORTHRUS_EINVAL, "x width")
     ws, ws_bytes = _room(workspace)
     dev = x.get_device()
     _here(dev, w, offsets, bias, workspace)
-    out = (rows, w.n)
+    out = (rows, n)
     e = None
     if bias is not None or act is not None or residual is not None:
         e = L.orthrus_epilogue()
@@ -210,7 +223,7 @@ def _product(w, x, offsets, y, bias, act, residual, workspace, stream):
             raise A.OrthrusError(A.ORTHRUS_EINVAL, "act")
         e.act = _ACTS[act]
         if bias is not None:
-            _need(bias.dtype == torch.float32 and bias.numel() == w.groups * (2 if w.gated else 1) * w.n and bias.shape[-1] == w.n and
+            _need(bias.dtype == torch.float32 and bias.numel() == groups * (2 if gated else 1) * n and bias.shape[-1] == n and
                   bias.is_contiguous(), "bias")
             e.bias = bias.data_ptr()
         if residual is not None:
@@ -239,5 +252,5 @@ def linear_grouped(w: LinearWeights, x: Rows, offsets: torch.Tensor, y: Rows, bi
     """`linear` of groups of rows: row r of [offsets[g], offsets[g + 1]) through the weights and bias ([groups][n], pairs
     [groups][2][n]) of group g.  offsets: int32 [groups + 1] on the device, ascending.  Rows of y outside all groups are left as they
     were."""
-    _need(offsets.dtype == torch.int32 and offsets.shape == (w.groups + 1,) and offsets.is_contiguous(), "offsets")
+    _need(offsets.dtype == torch.int32 and offsets.shape == (w._sizes[2] + 1,) and offsets.is_contiguous(), "offsets")
     _product(w, x, offsets, y, bias, act, residual, workspace, stream)
