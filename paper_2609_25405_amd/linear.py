@@ -167,6 +167,16 @@ def norm(x: torch.Tensor, y: Rows, gain: Optional[torch.Tensor] = None, eps: flo
         raise A.OrthrusError(rc, "orthrus_norm")
 
 
+def _lend(t: torch.Tensor, stream: Optional[int], dev: int) -> None:
+    """Makes memory just taken on the current stream safe to write on another: what used it before may still be queued, and it is
+    not given to others before the other stream is done with it."""
+    if stream is None or stream == _raw_stream(dev):
+        return
+    other = torch.cuda.ExternalStream(stream, device=dev) if stream else torch.cuda.default_stream(dev)
+    other.wait_stream(torch.cuda.current_stream(dev))
+    t.record_stream(other)
+
+
 class LinearWeights:
     """Weights in the layout that the products read, packed once from ``matrix`` [groups n][k] (bf16 tensor
     or Mx8), or, with ``up`` of the same shape and type, from a pair: y = act(x matrix^T) * (x up^T)."""
@@ -187,6 +197,7 @@ class LinearWeights:
         self._ref = byref(self._struct)
         self._sizes = (all_rows // groups, k, groups, up is not None)
         self._device = dev
+        _lend(self._packed, stream, dev)
         _check(L.load().orthrus_linear_pack(self._ref, m, second, _stream(stream, dev)), "orthrus_linear_pack")
 
     # bytes and sizes stay the ones that were packed
