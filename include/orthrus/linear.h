@@ -43,14 +43,14 @@ typedef struct orthrus_matrix {
 } orthrus_matrix;
 
 /* y = x in y's type, element by element: F32 or BF16 to MX8, or MX8 to F32 or BF16 (others
- * EUNSUPPORTED).  x and y share no memory.  Any strides >= width (scales: >= ceil(width / 32)) and any
+ * EUNSUPPORTED).  x and y share no memory (EINVAL).  Any strides >= width (scales: >= ceil(width / 32)) and any
  * alignment to an element. */
 int orthrus_convert(const orthrus_matrix *x, const orthrus_matrix *y, int32_t rows, int32_t width, void *stream);
 
 /* RMS norm of each row, after the addition of a residual: s = x + add (fp32; add NULL: s = x),
  * total = s rounded to its type (total NULL: not written), y = s * gain / sqrt(mean(s^2) + eps) in y's type
  * (gain fp32 device [width]; NULL: ones).  x, add, total: F32 or BF16; y: F32, BF16 or MX8.  total
- * may be x or add itself (data, stride and dtype); else what is written overlaps nothing.  The mean is taken in fp32 of the
+ * or y may be x or add itself (data, stride and dtype, not MX8); else what is written shares no byte with anything (EINVAL).  The mean is taken in fp32 of the
  * unrounded s (squares whose sum passes fp32's range make a row zero).  Any strides >= width
  *.  EINVAL: a null pointer, width < 1, eps
  * negative or not a number. */
@@ -70,12 +70,12 @@ typedef struct orthrus_linear_weights {
 size_t orthrus_linear_packed_bytes(const orthrus_linear_weights *w);
 
 /* Writes w->packed from [groups * n][k] matrices of w->dtype (`up` for gated weights, else NULL).  Any strides and
- * alignment to an element. */
+ * alignment to an element; packed shares no byte with them (EINVAL). */
 int orthrus_linear_pack(const orthrus_linear_weights *w, const orthrus_matrix *matrix, const orthrus_matrix *up, void *stream);
 
 /* What follows a product.  bias: fp32 device [groups][n] ([groups][2][n] for gated weights: those of the
  * activated matrix, then of the other), or NULL.  residual (data NULL: none): F32 or BF16 rows, added
- * last; may be y itself (data, stride and dtype), else y overlaps nothing that is read. */
+ * last; may be y itself (data, stride and dtype), else y and the workspace share no byte with anything (EINVAL). */
 typedef struct orthrus_epilogue {
     const float *bias;
     int32_t act;

@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "linear.hpp"
 #include "linear_mma.hpp"
@@ -191,6 +192,32 @@ Mat mat(const orthrus_matrix *m) {
     return Mat{(char *)m->data, (uint8_t *)m->scale, m->stride, m->scale_stride, m->dtype};
 }
 
+// what a call touches of a matrix: its elements, and the scales of 8-bit blocks
+Runs elements_of(const orthrus_matrix *m, int64_t rows, int32_t width) {
+    if (!m || !m->data) return Runs{0, 0, 0, 0};
+    const int64_t es = element_bytes(m->dtype);
+    return Runs{(__int128)(uintptr_t)m->data, (__int128)m->stride * es, (__int128)width * es, rows};
+}
+Runs scales_of(const orthrus_matrix *m, int64_t rows, int32_t width) {
+    if (!m || !m->data || m->dtype != ORTHRUS_MX8) return Runs{0, 0, 0, 0};
+    return Runs{(__int128)(uintptr_t)m->scale, m->scale_stride, (width + (int64_t)kBlock8 - 1) / kBlock8, rows};
+}
+Runs bytes_of(const void *p, size_t bytes) { return Runs{(__int128)(uintptr_t)p, 0, p ? (__int128)bytes : 0, 1}; }
+// one matrix: every element is read by the lane that writes it, before
+bool same_rows(const orthrus_matrix *a, const orthrus_matrix *b, int32_t rows) {
+    return a && b && a->data == b->data && a->dtype == b->dtype && a->dtype != ORTHRUS_MX8 && (rows == 1 || a->stride == b->stride);
+}
+// does what is written of y share memory with itself or with x?
+bool writes_meet(const orthrus_matrix *y, const Runs &x, int32_t rows, int32_t width) {
+    return runs_meet(elements_of(y, rows, width), x) || runs_meet(scales_of(y, rows, width), x);
+}
+bool writes_meet(const orthrus_matrix *y, const orthrus_matrix *x, int32_t rows, int32_t width, int32_t x_width) {
+    return writes_meet(y, elements_of(x, rows, x_width), rows, width) || writes_meet(y, scales_of(x, rows, x_width), rows, width);
+}
+bool meets_itself(const orthrus_matrix *y, int32_t rows, int32_t width) {
+    return runs_meet(elements_of(y, rows, width), scales_of(y, rows, width));
+}
+
 int product(const orthrus_linear_weights *w, const orthrus_matrix *x, const int32_t *offsets, bool grouped, int32_t rows,
             const orthrus_epilogue *e, const orthrus_matrix *y, void *workspace, size_t ws_bytes, void *stream) {
     if (!weights_ok(w) || rows < 0 || (!grouped && w->groups != 1)) return ORTHRUS_EINVAL;
@@ -216,6 +243,16 @@ int product(const orthrus_linear_weights *w, const orthrus_matrix *x, const int3
     const size_t need = slab_bytes(p.shape, rows, plan.splits);
     if (need > 0 && (!workspace || (uintptr_t)workspace % 16)) return ORTHRUS_EINVAL;
     if (ws_bytes < need) return ORTHRUS_ECAPACITY;
+    const Runs kept[] = {bytes_of(w->packed, orthrus_linear_packed_bytes(w)), bytes_of(grouped ? offsets : nullptr, ((size_t)w->groups + 1) * 4),
+                         bytes_of(e ? e->bias : nullptr, (size_t)w->groups * (w->gated ? 2 : 1) * w->n * 4)};
+    const Runs room = bytes_of(workspace, need);
+    const orthrus_matrix *res = e ? &e->residual : nullptr;
+    if (meets_itself(y, rows, w->n) || writes_meet(y, x, rows, w->n, w->k) || writes_meet(y, room, rows, w->n)) return ORTHRUS_EINVAL;
+    if (!same_rows(y, res, rows) && writes_meet(y, res, rows, w->n, w->n)) return ORTHRUS_EINVAL;
+    for (const Runs &r : kept)
+        if (writes_meet(y, r, rows, w->n) || runs_meet(room, r)) return ORTHRUS_EINVAL;
+    if (runs_meet(room, elements_of(x, rows, w->k)) || runs_meet(room, scales_of(x, rows, w->k)) || runs_meet(room, elements_of(res, rows, w->n)))
+        return ORTHRUS_EINVAL;
     p.w = (const char *)w->packed;
     p.group_bytes = (p.shape.bytes + 255) / 256 * 256;
     p.x = (const char *)x->data;
@@ -255,6 +292,7 @@ int orthrus_convert(const orthrus_matrix *x, const orthrus_matrix *y, int32_t ro
     if (!matrix_ok(x, width) || !matrix_ok(y, width)) return ORTHRUS_EINVAL;
     if ((x->dtype == ORTHRUS_MX8) == (y->dtype == ORTHRUS_MX8)) return ORTHRUS_EUNSUPPORTED;
     if (width > (1 << 30)) return ORTHRUS_ECAPACITY;
+    if (meets_itself(y, rows, width) || writes_meet(y, x, rows, width, width)) return ORTHRUS_EINVAL;
     return launch_convert(mat(x), mat(y), rows, width, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
 }
 
@@ -267,6 +305,13 @@ int orthrus_norm(const orthrus_matrix *x, const orthrus_matrix *add, const orthr
         return ORTHRUS_EINVAL;
     if (x->dtype == ORTHRUS_MX8 || (add && add->dtype == ORTHRUS_MX8) || (total && total->dtype == ORTHRUS_MX8)) return ORTHRUS_EUNSUPPORTED;
     if (width > (1 << 30)) return ORTHRUS_ECAPACITY;
+    const Runs factors = bytes_of(gain, (size_t)width * 4);
+    if (meets_itself(y, rows, width) || writes_meet(y, total, rows, width, width) || writes_meet(y, factors, rows, width) ||
+        writes_meet(total, factors, rows, width))
+        return ORTHRUS_EINVAL;
+    for (const orthrus_matrix *read : {x, add})
+        for (const orthrus_matrix *written : {y, total})
+            if (!same_rows(written, read, rows) && writes_meet(written, read, rows, width, width)) return ORTHRUS_EINVAL;
     const NormOp a{mat(x), mat(add), mat(total), mat(y), gain, eps, rows, width};
     return launch_norm_op(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
 }
@@ -284,6 +329,10 @@ int orthrus_linear_pack(const orthrus_linear_weights *w, const orthrus_matrix *m
     if (!weights_fit(w)) return ORTHRUS_ECAPACITY;
     PackedShape p = packed_shape(w->dtype, w->n, w->k, w->gated);
     p.bytes = (p.bytes + 255) / 256 * 256;
+    const Runs packed = bytes_of(w->packed, p.bytes * w->groups);
+    const int64_t rows = (int64_t)w->groups * w->n;
+    for (const orthrus_matrix *read : {matrix, up})
+        if (runs_meet(packed, elements_of(read, rows, w->k)) || runs_meet(packed, scales_of(read, rows, w->k))) return ORTHRUS_EINVAL;
     return launch_pack(*w, p, mat(matrix), mat(up), (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
 }
 

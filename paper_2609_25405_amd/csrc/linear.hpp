@@ -34,6 +34,36 @@ inline PackedShape packed_shape(int dtype, int n, int k, int gated) {
     return p;
 }
 
+// Runs of bytes, `stride` apart: what a call reads or writes of a matrix.
+struct Runs {
+    __int128 at, stride, bytes, rows;
+};
+// Do two share a byte?  Rows of one matrix often lie between those of another (columns of one buffer).
+constexpr bool runs_meet(Runs a, Runs b) {
+    if (a.rows < 1 || b.rows < 1 || a.bytes < 1 || b.bytes < 1) return false;
+    if (a.at + (a.rows - 1) * a.stride + a.bytes <= b.at || b.at + (b.rows - 1) * b.stride + b.bytes <= a.at) return false;
+    if (a.stride == b.stride && a.rows > 1 && b.rows > 1) {
+        // row j of b and row i of a share one where -b.bytes < b.at - a.at + (j - i) stride < a.bytes: the least such j - i, and
+        // is it one of two rows?
+        const __int128 least = a.at - b.at - b.bytes + 1, s = a.stride;
+        __int128 k = least >= 0 ? (least + s - 1) / s : -(-least / s);
+        if (k < 1 - a.rows) k = 1 - a.rows;
+        return k < b.rows && b.at - a.at + k * s < a.bytes;
+    }
+    if (a.rows > b.rows) {
+        const Runs c = a;
+        a = b;
+        b = c;
+    }
+    for (__int128 i = 0; i < a.rows; ++i) {
+        // the first row of b that ends behind where this one of a begins
+        const __int128 p = a.at + i * a.stride, past = p - b.at - b.bytes;
+        const __int128 j = past < 0 ? 0 : b.rows == 1 ? 1 : past / b.stride + 1;
+        if (j < b.rows && b.at + j * b.stride < p + a.bytes) return true;
+    }
+    return false;
+}
+
 // rows of a matrix, strides in elements (scales: bytes)
 struct Mat {
     char *data;

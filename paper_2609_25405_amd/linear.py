@@ -151,8 +151,8 @@ def convert(x: Rows, y: Rows, stream: Optional[int] = None) -> None:
 
 def norm(x: torch.Tensor, y: Rows, gain: Optional[torch.Tensor] = None, eps: float = 1e-5, add: Optional[torch.Tensor] = None,
          total: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
-    """RMS norm of the rows of s = x + add: y = s * gain / sqrt(mean(s^2) + eps), and total = s if given (it may
-    be x or add)."""
+    """RMS norm of the rows of s = x + add: y = s * gain / sqrt(mean(s^2) + eps), and total = s if given.  total or y
+    may be x or add; nothing else that is written may share memory with another argument."""
     shape = _shape2(x, "x")
     dev = x.get_device()
     _here(dev, gain)

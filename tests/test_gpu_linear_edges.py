@@ -44,3 +44,34 @@ def test_weights_packed_on_another_stream(side):
             after = torch.full_like(want, 9)
             torch.cuda.synchronize()
             assert (after == 9).all()
+
+
+# ------------------------------------------------------------------------------ memory that arguments share
+@pytest.mark.parametrize("width", [300, 301, 4096, 20000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("which", ["x", "add"])
+def test_norm_in_place(width, dtype, which):
+    """y over x or add, the total over the other one: the bits of the call that writes elsewhere."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(width)
+    rows = 1500 if width < 1000 else 20
+    a, b = (torch.randn((rows, width), generator=gen, device="cuda").to(dtype) for _ in range(2))
+    y, total = torch.empty_like(a), torch.empty_like(a)
+    L.norm(a, y, add=b, total=total)
+    c, d = a.clone(), b.clone()
+    L.norm(c, c if which == "x" else d, add=d, total=d if which == "x" else c)
+    assert torch.equal(c if which == "x" else d, y) and torch.equal(d if which == "x" else c, total)
+
+
+def test_columns_of_one_buffer():
+    """x, residual and y side by side in the rows of one buffer share no byte."""
+    room = torch.randn((200, 3 * 128), device="cuda").to(torch.bfloat16)
+    before = room.clone()
+    x, res, y = room[:, :128], room[:, 128:256], room[:, 256:]
+    w = L.LinearWeights(torch.randn((128, 128), device="cuda").to(torch.bfloat16))
+    L.linear(w, x, y, residual=res)
+    apart = torch.empty((200, 128), dtype=torch.bfloat16, device="cuda")
+    L.linear(w, x.contiguous(), apart, residual=res.contiguous())
+    assert torch.equal(y, apart) and torch.equal(room[:, :256], before[:, :256])
+    with pytest.raises(L.A.OrthrusError):
+        L.linear(w, x, room[:, 64:192])
