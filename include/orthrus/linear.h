@@ -66,7 +66,7 @@ typedef struct orthrus_linear_weights {
     int32_t n, k, gated, groups;
 } orthrus_linear_weights;
 
-/* Bytes of packed weights (`packed` is not looked at; 0 for invalid sizes). */
+/* Bytes of packed weights (`packed` is not looked at; 0 for invalid sizes, k > 2^22 and n > 2^26). */
 size_t orthrus_linear_packed_bytes(const orthrus_linear_weights *w);
 
 /* Writes w->packed from [groups * n][k] matrices of w->dtype (`up` for gated weights, else NULL).  Any strides and
@@ -93,8 +93,9 @@ size_t orthrus_linear_bytes(const orthrus_linear_weights *w, int32_t rows);
  * none.  Sums in fp32, in an order that depends on the sizes alone; bf16 products are exact.  The matrix cores add 8-bit
  * products eight neighbours at a time, without the bits below 2^-13 of the power of two of the largest of the eight.
  * workspace: 16-byte aligned, one call in flight; calls may be captured into graphs.  EINVAL: null pointers, sizes, strides or
- * alignments against the above; EUNSUPPORTED: types without a kernel; ECAPACITY: workspace too small, or more than 2^31
- * bytes in a row tile's rows.  rows = 0 is a no-op. */
+ * alignments against the above; EUNSUPPORTED: types without a kernel; ECAPACITY: workspace too small; k > 2^22,
+ * n > 2^26 or rows >= 2^30; 2^31 bytes or more in 256 rows of x or of its scales; more tiles than a launch holds (2^24 of 64 rows by 128
+ * weight rows or more; 2^23 of 16 by 16 or more where a group's share is at most 16 rows).  rows = 0 is a no-op. */
 int orthrus_linear(const orthrus_linear_weights *w, const orthrus_matrix *x, int32_t rows, const orthrus_epilogue *epilogue,
                    const orthrus_matrix *y, void *workspace, size_t ws_bytes, void *stream);
 

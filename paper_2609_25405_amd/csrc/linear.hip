@@ -84,6 +84,7 @@ hipError_t launch_pack(const orthrus_linear_weights &w, const PackedShape &p, co
 namespace {
 constexpr int kMostSplits = 8;
 constexpr size_t kMostSlab = (size_t)64 << 20;
+constexpr int32_t kMostRows = 1 << 30;    // a row tile's end stays an int
 constexpr int kCus = 256;
 int div_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
@@ -116,7 +117,7 @@ int64_t most_row_tiles(int64_t rows, int64_t groups, int bm) {
     return groups == 1 ? (rows + bm - 1) / bm : std::min(rows, rows / bm + std::min(rows, groups));
 }
 
-int few_units(const PackedShape &s, int rows, int groups, int nt) { return (int)(div_up(s.tiles, nt) * most_row_tiles(rows, groups, 16)); }
+int64_t few_units(const PackedShape &s, int rows, int groups, int nt) { return div_up(s.tiles, nt) * most_row_tiles(rows, groups, 16); }
 int few_tiles(const PackedShape &s, int rows, int groups, int gated, int y_dtype) {
     // Whole units of output, and more (so that x is read less often) while three quarters of the CUs have work: 16 x 6144 x 4096 in 8
     // bits 7.4 us with two tiles a workgroup, 9.6 with one; one row 6.8 with either
@@ -177,7 +178,7 @@ bool weights_ok(const orthrus_linear_weights *w) {
     return w && (w->dtype == ORTHRUS_BF16 || w->dtype == ORTHRUS_MX8) && w->n > 0 && w->k > 0 && w->groups > 0 &&
            (w->gated == 0 || w->gated == 1);
 }
-// sizes that the kernels' 32-bit offsets hold: a tile's rows of the weights, all tiles' units
+// sizes that the kernels' 32-bit offsets hold: a workgroup's tiles of the weights, all tiles' columns
 bool weights_fit(const orthrus_linear_weights *w) { return w->k <= (1 << 22) && w->n <= (1 << 26); }
 
 size_t element_bytes(int dtype) { return dtype == ORTHRUS_F32 ? 4 : dtype == ORTHRUS_BF16 ? 2 : 1; }
@@ -235,11 +236,14 @@ int product(const orthrus_linear_weights *w, const orthrus_matrix *x, const int3
             if (e->residual.dtype == ORTHRUS_MX8) return ORTHRUS_EUNSUPPORTED;
         }
     }
+    if (!weights_fit(w) || rows >= kMostRows || xs > 0x7fffffff / 256 || x->scale_stride > 0x7fffffff / 256) return ORTHRUS_ECAPACITY;
     Product p{};
     p.shape = packed_shape(w->dtype, w->n, w->k, w->gated);
-    if (!weights_fit(w) || xs > 0x7fffffff / 256 || x->scale_stride > 0x7fffffff / 256) return ORTHRUS_ECAPACITY;
     const ProductPlan plan = plan_product(p.shape, rows, w->groups, !grouped);
-    if ((int64_t)plan.m_tiles_most * p.shape.tiles > (1 << 22)) return ORTHRUS_ECAPACITY;
+    // (a launch holds fewer than 2^32 threads in a direction)
+    if (plan.shape < 0 ? few_units(p.shape, rows, w->groups, few_tiles(p.shape, rows, w->groups, w->gated, y->dtype)) >= (1 << 23)
+                       : plan.m_tiles_most * (int64_t)div_up(p.shape.tiles, kTiles[plan.shape].bn / 16) >= (1 << 24))
+        return ORTHRUS_ECAPACITY;
     const size_t need = slab_bytes(p.shape, rows, plan.splits);
     if (need > 0 && (!workspace || (uintptr_t)workspace % 16)) return ORTHRUS_EINVAL;
     if (ws_bytes < need) return ORTHRUS_ECAPACITY;

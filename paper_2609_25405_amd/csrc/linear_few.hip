@@ -101,7 +101,7 @@ template <int DT, int NT, int DEPTH, bool GATED> __global__ __launch_bounds__(64
 
 template <int DT, int NT, bool GATED> hipError_t go(const Product &p, hipStream_t s) {
     constexpr int DEPTH = NT == 4 ? 3 : 4;
-    hipLaunchKernelGGL((few_kernel<DT, NT, DEPTH, GATED>), dim3(few_units(p.shape, p.rows, p.groups, NT)), dim3(64 * kWaves), 0, s, p);
+    hipLaunchKernelGGL((few_kernel<DT, NT, DEPTH, GATED>), dim3((unsigned)few_units(p.shape, p.rows, p.groups, NT)), dim3(64 * kWaves), 0, s, p);
     return hipGetLastError();
 }
 template <int DT> hipError_t go_tiles(const Product &p, hipStream_t s) {

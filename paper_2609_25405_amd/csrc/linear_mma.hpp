@@ -64,7 +64,7 @@ __device__ __forceinline__ void mma_half_step(f32x16 &acc, i32x8 w, i32x8 x, int
 
 // the weight tiles that a workgroup of linear_few.hip owns, and how many workgroups there can be
 int few_tiles(const PackedShape &s, int rows, int groups, int gated, int y_dtype);
-int few_units(const PackedShape &s, int rows, int groups, int nt);
+int64_t few_units(const PackedShape &s, int rows, int groups, int nt);
 // row tiles of bm rows that `rows` rows in `groups` groups can have
 int64_t most_row_tiles(int64_t rows, int64_t groups, int bm);
 

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2609_25405_amd import linear as L
+from tests.linear_common import check, host, product_bound
 
 pytestmark = pytest.mark.gpu
 
@@ -75,3 +76,19 @@ def test_columns_of_one_buffer():
     assert torch.equal(y, apart) and torch.equal(room[:, :256], before[:, :256])
     with pytest.raises(L.A.OrthrusError):
         L.linear(w, x, room[:, 64:192])
+
+
+# ------------------------------------------------------------------------------ sizes
+@pytest.mark.parametrize("rows,n,k,gated", [((1 << 28) + 5, 16, 16, False), ((1 << 20) + 3, 14336, 32, True)])
+def test_millions_of_tiles(rows, n, k, gated):
+    """More than 2^22 tiles of 16 weight rows by a workgroup's rows."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(7)
+    x = torch.empty((rows, k), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    ws = [torch.randn((n, k), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(1 + gated)]
+    y = torch.full((rows, n), -77.0, dtype=torch.bfloat16, device="cuda")
+    w = L.LinearWeights(ws[0], up=ws[1] if gated else None)
+    L.linear(w, x, y, act="silu" if gated else None, workspace=L.linear_workspace(w, rows))
+    at = torch.tensor([0, 1, 255, 256, 65535, rows // 2, rows // 2 + 77, rows - 257, rows - 2, rows - 1], device="cuda")
+    want, bound = product_bound(host(x[at]), host(ws[0]), host(ws[1]) if gated else None, None, "silu" if gated else None, None, "bf16")
+    check(y[at], want, bound, (rows, n, k))

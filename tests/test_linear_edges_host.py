@@ -188,3 +188,27 @@ def test_rows_that_share_nothing_pass():
         linear = lambda y, res=None: lib.orthrus_linear(ref(w), ref(x), 8, ref(B.orthrus_epilogue(AT[4], 0, res or B.orthrus_matrix())), ref(y), None, 0, None)
         assert linear(rows(1)) == linear(rows(1), rows(1)) == linear(rows(1, MX8), rows(2)) == passed
         assert linear(rows(0, stride=128 // (1 + mx), off=128)) == (A.ORTHRUS_EINVAL if mx else passed)
+
+
+# ------------------------------------------------------------------------------ sizes
+@pytest.mark.parametrize("R,N,K,groups", [(1 << 30, 1, 1, 1), ((1 << 31) - 1, 1, 1, 1), ((1 << 31) - 1, 1, 1, 1 << 28), (3, (1 << 26) + 1, 64, 1),
+                                          (3, (1 << 31) - 1, 64, 1), (3, (1 << 31) - 15, 64, 1), (3, 1, (1 << 22) + 1, 1), (3, 1, (1 << 31) - 1, 1),
+                                          ((1 << 30) - 1, 2048, 64, 1), ((1 << 30) - 1, 64, 64, 1 << 27)])
+def test_sizes_past_a_launch_are_refused(R, N, K, groups):
+    lib = B.load()
+    w = B.orthrus_linear_weights(1 << 40, BF16, N, K, 0, groups)
+    x, y = B.orthrus_matrix(1 << 60, None, -(-K // 8) * 8, 0, BF16), B.orthrus_matrix(1 << 61, None, N, 0, BF16)
+    args = [] if groups == 1 else [1 << 20]
+    f = lib.orthrus_linear if groups == 1 else lib.orthrus_linear_grouped
+    assert f(ref(w), ref(x), *args, R, None, ref(y), 1 << 59, 1 << 40, None) == A.ORTHRUS_ECAPACITY
+    if K > 1 << 22 or N > 1 << 26:
+        assert lib.orthrus_linear_packed_bytes(ref(w)) == lib.orthrus_linear_bytes(ref(w), 3) == 0
+        assert lib.orthrus_linear_pack(ref(w), ref(B.orthrus_matrix(1 << 60, None, K, 0, BF16)), None, None) == A.ORTHRUS_ECAPACITY
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the calls below pass the host's checks")
+@pytest.mark.parametrize("R,N,gated", [(1 << 20, 14336, 1), (1 << 28, 16, 0), (4 << 20, 14336, 0), (200000, 1 << 20, 0)])
+def test_sizes_that_a_launch_holds_pass(R, N, gated):
+    w = B.orthrus_linear_weights(1 << 40, BF16, N, 64, gated, 1)
+    x, y = B.orthrus_matrix(1 << 60, None, 64, 0, BF16), B.orthrus_matrix(1 << 61, None, N, 0, BF16)
+    assert B.load().orthrus_linear(ref(w), ref(x), R, None, ref(y), None, 0, None) == A.ORTHRUS_EHIP
