@@ -82,8 +82,8 @@ typedef struct orthrus_epilogue {
     orthrus_matrix residual;
 } orthrus_epilogue;
 
-/* Device workspace bytes of a product of up to `rows` rows (the same bound serves every smaller
- * number of rows; 0: none is needed, or invalid arguments). */
+/* Device workspace bytes that hold what a product of up to `rows` rows may need (the same bound serves every smaller
+ * number of rows; at most 64 MiB; 0: none is needed, or invalid arguments). */
 size_t orthrus_linear_bytes(const orthrus_linear_weights *w, int32_t rows);
 
 /* y[r] = act(x[r] W^T + bias) + residual[r], or for gated weights act(x W^T + bias) * (x U^T + bias_u) +

@@ -82,7 +82,7 @@ hipError_t launch_pack(const orthrus_linear_weights &w, const PackedShape &p, co
 
 // ------------------------------------------------------------------------------ covers
 namespace {
-constexpr int kMostSplits = 8;
+constexpr int kMostSplits = 8, kLeastSteps = 4;     // parts of K, and steps of a part
 constexpr size_t kMostSlab = (size_t)64 << 20;
 constexpr int32_t kMostRows = 1 << 30;    // a row tile's end stays an int
 constexpr int kCus = 256;
@@ -111,6 +111,18 @@ double tiles_us(const TileShape &t, double n, double steps) {
 }  // namespace
 
 size_t slab_bytes(const PackedShape &s, int rows, int splits) { return splits > 1 ? (size_t)splits * rows * s.tiles * 64 : 0; }
+
+// the most sums that plan_product leaves in a workspace, over all numbers of rows up to `rows`: what keeps it from cutting K, without
+// its estimates
+size_t most_slab(const PackedShape &s, int rows) {
+    size_t most = 0;
+    for (int split = 2; split <= kMostSplits && s.steps / split >= kLeastSteps; ++split)
+        for (const TileShape &t : kTiles) {
+            const int64_t cut = (int64_t)(2 * kCus - 1) / (split - 1) / div_up(s.tiles, t.bn / 16) * t.bm;     // the most rows in so many parts
+            most = std::max(most, std::min(slab_bytes(s, (int)std::min<int64_t>(rows, cut), split), kMostSlab));
+        }
+    return most;
+}
 
 // a group of rows takes at most one tile more than its share
 int64_t most_row_tiles(int64_t rows, int64_t groups, int bm) {
@@ -142,7 +154,7 @@ ProductPlan plan_product(const PackedShape &s, int rows, int groups, bool joint)
         const double tiles = m_tiles * div_up(s.tiles, t.bn / 16);
         for (int split = 1; split <= (joint ? kMostSplits : 1); ++split) {
             // (more parts than two rounds of tiles only cost)
-            if (split > 1 && (s.steps / split < 4 || slab_bytes(s, rows, split) > kMostSlab || tiles * (split - 1) >= 2 * kCus)) break;
+            if (split > 1 && (s.steps / split < kLeastSteps || slab_bytes(s, rows, split) > kMostSlab || tiles * (split - 1) >= 2 * kCus)) break;
             const double tile_us = tiles_us(t, tiles * split, div_up(s.steps, split));
             double us = std::max(tile_us, weight_us) + kUnhidden * std::min(tile_us, weight_us);
             if (split > 1) us += kJoinUs + 2.0 * slab_bytes(s, rows, split) / kBytesPerUs;
@@ -342,8 +354,7 @@ int orthrus_linear_pack(const orthrus_linear_weights *w, const orthrus_matrix *m
 
 size_t orthrus_linear_bytes(const orthrus_linear_weights *w, int32_t rows) {
     if (!weights_ok(w) || !weights_fit(w) || rows < 1 || w->groups != 1) return 0;
-    const PackedShape s = packed_shape(w->dtype, w->n, w->k, w->gated);
-    return std::min(slab_bytes(s, rows, kMostSplits), kMostSlab);
+    return most_slab(packed_shape(w->dtype, w->n, w->k, w->gated), rows);
 }
 
 int orthrus_linear(const orthrus_linear_weights *w, const orthrus_matrix *x, int32_t rows, const orthrus_epilogue *epilogue,

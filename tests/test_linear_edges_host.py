@@ -212,3 +212,45 @@ def test_sizes_that_a_launch_holds_pass(R, N, gated):
     w = B.orthrus_linear_weights(1 << 40, BF16, N, 64, gated, 1)
     x, y = B.orthrus_matrix(1 << 60, None, 64, 0, BF16), B.orthrus_matrix(1 << 61, None, N, 0, BF16)
     assert B.load().orthrus_linear(ref(w), ref(x), R, None, ref(y), None, 0, None) == A.ORTHRUS_EHIP
+
+
+class PackedShape(ctypes.Structure):
+    _fields_ = [("tiles", ctypes.c_int), ("steps", ctypes.c_int), ("quads", ctypes.c_int), ("tile_bytes", ctypes.c_size_t),
+                ("scale_at", ctypes.c_size_t), ("bytes", ctypes.c_size_t)]
+
+
+class ProductPlan(ctypes.Structure):
+    _fields_ = [("shape", ctypes.c_int), ("splits", ctypes.c_int), ("m_tiles_most", ctypes.c_int)]
+
+
+def packed_shape(dtype, n, k, gated):
+    tiles, steps = -(-n // 16) * (2 if gated else 1), -(-k * (1 if dtype == MX8 else 2) // 128)
+    at = tiles * steps * 2048
+    return PackedShape(tiles, steps, -(-tiles // 4), steps * 2048, at, at + (-(-tiles // 4) * steps * 256 if dtype == MX8 else 0))
+
+
+def cover(dtype, rows, n, k, gated=False, groups=1):
+    """The cover that a product takes (shape of tiles or -1, parts of K)."""
+    f = B.load()["_ZN7orthrus12plan_productERKNS_11PackedShapeEiib"]
+    f.restype, f.argtypes = ProductPlan, [ctypes.POINTER(PackedShape), ctypes.c_int, ctypes.c_int, ctypes.c_bool]
+    return f(packed_shape(dtype, n, k, gated), rows, groups, groups == 1)
+
+
+@pytest.mark.parametrize("dtype", [BF16, MX8])
+@pytest.mark.parametrize("n", [1, 48, 1000, 4096, 14336, 32000, 200000])
+@pytest.mark.parametrize("gated", [0, 1])
+def test_workspaces_hold_every_smaller_call_and_only_cut_sums_need_one(dtype, n, gated):
+    cut = 0
+    for k in (64, 400, 1000, 4096, 14336, 65536):
+        w = B.orthrus_linear_weights(None, dtype, n, k, gated, 1)
+        room = lambda rows: B.load().orthrus_linear_bytes(ref(w), rows)
+        shape, most = packed_shape(dtype, n, k, gated), 0
+        for rows in list(range(1, 70)) + list(range(70, 700, 37)) + [1024, 1280, 2000, 4096, 5000, 8192, 100000]:
+            plan = cover(dtype, rows, n, k, gated)
+            if plan.splits > 1:
+                most = max(most, plan.splits * rows * shape.tiles * 64)
+                cut += 1
+            assert most <= room(rows) <= 64 << 20, (k, rows)
+        if shape.steps < 8 or n > 150000:            # parts of fewer than four steps, or more tiles than two rounds: never cut
+            assert room(8192) == room(1) == 0
+    assert cut > 0 or n > 20000
