@@ -1,5 +1,7 @@
 """Norms and products on the GPU: memory that streams hand to one another, in place calls, scales that no rounding makes, and
 more work than small grids hold."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -92,3 +94,33 @@ def test_millions_of_tiles(rows, n, k, gated):
     at = torch.tensor([0, 1, 255, 256, 65535, rows // 2, rows // 2 + 77, rows - 257, rows - 2, rows - 1], device="cuda")
     want, bound = product_bound(host(x[at]), host(ws[0]), host(ws[1]) if gated else None, None, "silu" if gated else None, None, "bf16")
     check(y[at], want, bound, (rows, n, k))
+
+
+# ------------------------------------------------------------------------------ activations
+# Bounds relative to the result, u = 2^-24 (a hardware exponential or reciprocal is off by 2 u at most).
+# over 1 + exp(-a): the argument a log2(e) is rounded once and its constant by less than u / 2 of itself, 1.5 |a| u; exponential and
+#   reciprocal 4 u, a sum and a product 2 u: (6 + 1.5 |a|) u.  The tanh form's argument takes five roundings more: 5 |a| u.
+# gelu: q's polynomial 1.2e-7 = 2 u; nine steps of Horner, each at most the sum of the coefficients' magnitudes over the value,
+#   0.93 / 0.5, off: 17 u; the reciprocal's 2 u (and its argument's u) through a slope of the logarithm of at most sum i |c_i| / 0.5 = 8: 24 u; two roundings
+#   and the constant's of the exponent, v^2 / 2 of them each: 1.25 v^2 u; exponential, two products, a sum: 5 u.
+@pytest.mark.parametrize("act,limit", [("silu", lambda v: 6 + 1.5 * np.abs(v)), ("gelu", lambda v: 48 + 1.25 * v * v),
+                                       ("gelu_tanh", lambda v: 6 + 6.5 * 1.6 * np.abs(v + 0.044715 * v ** 3))])
+@pytest.mark.parametrize("rows", [3, 70])
+def test_activations_of_far_values(act, limit, rows):
+    """Values from the bias alone, out to where the results are tiny: relative to the results."""
+    n = 4096
+    far = {"silu": 80, "gelu": 12.9, "gelu_tanh": 9}[act]
+    v = np.linspace(-far, far, n).astype(np.float32)
+    w = L.LinearWeights(torch.ones((n, 16), dtype=torch.bfloat16, device="cuda"))
+    y = torch.empty((rows, n), device="cuda")
+    L.linear(w, torch.zeros((rows, 16), dtype=torch.bfloat16, device="cuda"), y, bias=torch.tensor(v, device="cuda"), act=act, workspace=L.linear_workspace(w, rows))
+    v = v.astype(np.float64)
+    if act == "gelu":
+        want = v * 0.5 * np.array([math.erfc(-c / math.sqrt(2)) for c in v])
+    else:
+        want = v / (1 + np.exp(-(v if act == "silu" else 2 * math.sqrt(2 / math.pi) * (v + 0.044715 * v ** 3))))
+    got = host(y)
+    assert (got == got[0]).all()
+    off = np.abs(got[0] - want) / (limit(v) * 2.0 ** -24 * np.abs(want) + 1e-37)
+    assert off.max() <= 1, (v[off.argmax()], off.max())
+    print(act, "largest part of the bound", off.max())
