@@ -7,7 +7,8 @@
  * 8-bit blocks (ORTHRUS_MX8).  32 consecutive elements of a row (the last ones of a row may be
  * fewer) share a power-of-two scale, held as its biased exponent in one byte: 2^(byte - 127), 255 is
  * not a number.  An element is an e4m3 code (4 exponent, 3 mantissa bits, largest value 448, no
- * infinities) times its block's scale, so its value is exact in bfloat16.
+ * infinities) times its block's scale: exact in fp32 under bytes up to 246, in bfloat16 under bytes 3 to 246 (rounding to blocks
+ * writes bytes 27 to 247, and no value past fp32's range).
  *   - Rounding to blocks takes the least scale 2^e (e >= -100) with max |x| <= 448 * 2^e over the
  *     block's finite elements, and the nearest code, ties to even.
  *   - Elements that are infinite or not a number, or that would round to 2^128, become the code of

@@ -139,7 +139,8 @@ def _shape2(t: Rows, what: str):
 
 
 def convert(x: Rows, y: Rows, stream: Optional[int] = None) -> None:
-    """y = x in y's type: fp32 or bf16 rows to 8-bit blocks, or back (exact in bf16)."""
+    """y = x in y's type: fp32 or bf16 rows to 8-bit blocks, or back (rounded; what fp32 or bf16
+    rows became is exact in either)."""
     shape = _shape2(x, "x")
     dev = x.get_device()
     _here(dev)

@@ -124,3 +124,46 @@ def test_activations_of_far_values(act, limit, rows):
     off = np.abs(got[0] - want) / (limit(v) * 2.0 ** -24 * np.abs(want) + 1e-37)
     assert off.max() <= 1, (v[off.argmax()], off.max())
     print(act, "largest part of the bound", off.max())
+
+
+# ------------------------------------------------------------------------------ scales of any byte
+def blocks_of(codes, scales):
+    """Mx8 of uint8 arrays."""
+    to = lambda a: torch.tensor(np.ascontiguousarray(a), dtype=torch.uint8, device="cuda")
+    return L.Mx8.of(to(codes).view(torch.float8_e4m3fn), to(scales))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_read_back_of_every_code_under_every_scale(dtype):
+    """The value, rounded to the type read into: exact in fp32 under bytes up to 246, in bfloat16 under bytes 3 to 246."""
+    codes = np.tile(np.arange(256, dtype=np.uint8), (256, 1))
+    scales = np.tile(np.arange(256, dtype=np.uint8)[:, None], (1, 8))
+    m = blocks_of(codes, scales)
+    y = torch.empty((256, 256), dtype=dtype, device="cuda")
+    L.convert(m, y)
+    code = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy().astype(np.float64)
+    exact = code[None] * 2.0 ** (np.arange(256, dtype=np.float64)[:, None] - 127)
+    exact[255] = np.nan
+    want = torch.tensor(exact).to(torch.float32).to(dtype).double().numpy()
+    got = host(y)
+    bad = ~((got == want) | (np.isnan(got) & np.isnan(want)))
+    assert not bad.any(), [(int(r), hex(int(c)), got[r, c], want[r, c]) for r, c in np.argwhere(bad)[:5]]
+    sure = slice(0 if dtype == torch.float32 else 3, 247)
+    assert np.array_equal(got[sure], exact[sure], equal_nan=True)
+
+
+@pytest.mark.parametrize("rows", [7, 80])
+@pytest.mark.parametrize("a,b", [(0, 254), (254, 0), (1, 250), (100, 154), (3, 130), (246, 1)])
+def test_products_under_far_scales(rows, a, b):
+    """Scales of x and of the weights at the ends of their range, whose product is ordinary."""
+    rng = np.random.default_rng(a)
+    code = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy().astype(np.float64)
+    fine = np.flatnonzero(np.isfinite(code) & (np.abs(code) >= 2.0 ** -6) & (np.abs(code) < 16))
+    cx, cw = (rng.choice(fine, (r, 160)).astype(np.uint8) for r in (rows, 48))
+    x, m = blocks_of(cx, np.full((rows, 5), a)), blocks_of(cw, np.full((48, 5), b))
+    y = torch.empty((rows, 48), device="cuda")
+    w = L.LinearWeights(m)
+    L.linear(w, x, y, workspace=L.linear_workspace(w, rows))
+    scale = 2.0 ** (a + b - 254)
+    want, bound = product_bound(code[cx], code[cw], None, None, None, None, "mx8")
+    check(y, want * scale, bound * scale, (a, b))
