@@ -136,13 +136,18 @@ __global__ __launch_bounds__(NT) void norm_op_kernel(NormOp a) {
         }
     } else {
         for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-            float s[8], g[8], sq = 0.f;
+            // (runs of eight are added in two parts: a thread has any number of them, and in fp32 a row of 2^24 equal elements would be off
+            // by up to a thousandth)
+            float s[8], g[8];
+            Two whole{0.f, 0.f};
             for (int col = 8 * t; col < a.width; col += 8 * NT) {
                 sum_at(row, col, s);
+                float sq = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sq = fmaf(s[i], s[i], sq);
+                whole = add(whole, Two{sq, 0.f});
             }
-            const Two f = factor(sq, turn++);
+            const Two f = factor(isfinite(whole.high) ? whole.high + whole.low : whole.high, turn++);
             for (int c0 = 0; c0 < a.width; c0 += 8 * NT) {
                 const int col = c0 + 8 * t;
                 const bool in = col < a.width;

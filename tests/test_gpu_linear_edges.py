@@ -167,3 +167,30 @@ def test_products_under_far_scales(rows, a, b):
     scale = 2.0 ** (a + b - 254)
     want, bound = product_bound(code[cx], code[cw], None, None, None, None, "mx8")
     check(y, want * scale, bound * scale, (a, b))
+
+
+# ------------------------------------------------------------------------------ wide rows
+@pytest.mark.parametrize("width", [16384, 16385, 1 << 20, (1 << 24) + 3])
+@pytest.mark.parametrize("value", [1.0, 1.0437, 1.3, None])
+def test_norm_of_wide_rows(width, value):
+    """A row's squares are sixteen or fewer additions in fp32 deep, four more between lanes, halved by the root; the factor's and the products'
+    roundings are three: 2^-20 of the value (u = 2^-24), whatever the width.  Equal elements are the worst for longer sums, whose
+    roundings then all fall on one side."""
+    x = torch.full((2, width), value or 0.0, device="cuda")
+    if value is None:
+        x.normal_(generator=torch.Generator(device="cuda").manual_seed(3))
+    y = torch.empty_like(x)
+    L.norm(x, y)
+    s = x.double()
+    want = s / (s.square().mean(-1, keepdim=True) + 1e-5).sqrt()
+    assert ((y.double() - want).abs() <= 2.0 ** -20 * want.abs()).all(), float(((y.double() - want).abs() / want.abs()).max() * 2 ** 24)
+
+
+def test_wide_rows_past_the_range():
+    """Squares whose sum passes fp32's range make a row zero, not a number makes it so, of wide rows as of narrow ones."""
+    for width in (4096, 40000):
+        x = torch.ones((3, width), device="cuda")
+        x[0], x[1, width - 1] = 1e20, float("nan")
+        y = torch.full_like(x, 5.0)
+        L.norm(x, y)
+        assert (y[0] == 0).all() and y[1].isnan().all() and ((y[2] - 1).abs() < 1e-4).all()
