@@ -52,9 +52,10 @@ int orthrus_convert(const orthrus_matrix *x, const orthrus_matrix *y, int32_t ro
 /* RMS norm of each row, after the addition of a residual: s = x + add (fp32; add NULL: s = x),
  * total = s rounded to its type (total NULL: not written), y = s * gain / sqrt(mean(s^2) + eps) in y's type
  * (gain fp32 device [width]; NULL: ones).  x, add, total: F32 or BF16; y: F32, BF16 or MX8.  total
- * or y may be x or add itself (data, stride and dtype, not MX8); else what is written shares no byte with anything (EINVAL).  The mean is that of the
- * unrounded sums' squares in fp32, short sums of which are added in two parts: y is off by at most 2^-20 of itself, and half a step of
- * its type (squares whose sum passes fp32's range make a row zero).  Any strides >= width and any alignment to an element.
+ * or y may be x or add itself (data, stride and dtype, not MX8); else what is written shares no byte with anything (EINVAL).  The mean is taken in 64
+ * bits of s as fp32 holds it: y is off by at most 2^-22 of itself, and half a step of its type (squares whose sum passes fp32's range make a row
+ * zero; 8-bit codes with three bits of mantissa are rounded once, from s before
+ * its rounding).  Any strides >= width and any alignment to an element.
  * EINVAL: a null pointer, width < 1, eps negative or not a number; ECAPACITY: width > 2^30. */
 int orthrus_norm(const orthrus_matrix *x, const orthrus_matrix *add, const orthrus_matrix *total, const float *gain, float eps,
                  const orthrus_matrix *y, int32_t rows, int32_t width, void *stream);

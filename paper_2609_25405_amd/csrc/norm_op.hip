@@ -7,36 +7,43 @@ namespace orthrus {
 namespace {
 
 #if defined(__HIP_DEVICE_COMPILE__)
-// A value in two parts, high + low: a row's statistics where they are large, so that what all its elements share is off by less than
-// their own rounding
+// A value in two parts, high + low: a row's factor, so that it adds nothing to its elements' own roundings, and an element that is
+// formed again (in 64 bits the operands would take half as many registers more, kept for a branch that is hardly taken: 42 us for 30)
 struct Two {
     float high, low;
 };
-__device__ __forceinline__ Two add(Two a, Two b) {
-    const float s = a.high + b.high, t = s - a.high;
-    return Two{s, (a.high - (s - t)) + (b.high - t) + (a.low + b.low)};
+__device__ __forceinline__ Two add(float a, float b) {
+    const float s = a + b, t = s - a;
+    return Two{s, (a - (s - t)) + (b - t)};
 }
-// the sum of all threads' v (small sums in fp32, the last ones in two parts); two calls in a row are given different places
-template <int NT> __device__ __forceinline__ Two block_sum(float v, Two *shared) {
-#pragma unroll
-    for (int o = 32; o >= 4; o >>= 1) v += __shfl_xor(v, o, 64);
-    Two s = add(Two{v, 0.f}, Two{quad_lane<0xB1>(v), 0.f});
-    s = add(s, Two{quad_lane<0x4E>(s.high), quad_lane<0x4E>(s.low)});
-    if constexpr (NT == 64) return s;
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = s;
+template <int CTRL> __device__ __forceinline__ double other_lane(double v) {
+    const uint64_t b = (uint64_t)__double_as_longlong(v);
+    const uint32_t lo = __builtin_amdgcn_mov_dpp((uint32_t)b, CTRL, 0xf, 0xf, true), hi = __builtin_amdgcn_mov_dpp((uint32_t)(b >> 32), CTRL, 0xf, 0xf, true);
+    return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+// the sum of all threads' v; two calls in a row are given different places
+template <int NT> __device__ __forceinline__ double block_sum(double v, double *shared) {
+    v += __shfl_xor(v, 32, 64);
+    v += __shfl_xor(v, 16, 64);
+    v += other_lane<0x140>(v);      // 15 - lane of 16, 7 - lane of 8, the neighbouring pair, the neighbour
+    v += other_lane<0x141>(v);
+    v += other_lane<0x4E>(v);
+    v += other_lane<0xB1>(v);
+    if constexpr (NT == 64) return v;
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
     __syncthreads();
-    s = shared[0];
+    v = shared[0];
 #pragma unroll
-    for (int i = 1; i < NT / 64; ++i) s = add(s, shared[i]);
-    return s;
+    for (int i = 1; i < NT / 64; ++i) v += shared[i];
+    return v;
 }
-// 1 / sqrt(sum / width + eps)
-__device__ __forceinline__ Two row_factor(Two sum, float width, float eps) {
-    const float q = sum.high / width, rest = (fmaf(-q, width, sum.high) + sum.low) * __builtin_amdgcn_rcpf(width);
-    const Two m = add(Two{q, rest}, Two{eps, 0.f});
-    const float f = 1.f / sqrtf(m.high), t = f * f;
-    const float e = fmaf(-t, m.high, 1.f) - fmaf(f, f, -t) * m.high - t * m.low;       // 1 - f^2 m
-    return Two{f, isfinite(e) ? 0.5f * e * f : 0.f};
+// 1 / sqrt(sum / width + eps), share = 1 / width.  A sum past fp32's range is infinite.
+__device__ __forceinline__ Two row_factor(double sum, double share, float eps) {
+    if (!(sum <= 0x1.fffffep127)) sum = (float)sum;
+    const double m = fma(sum, share, (double)eps);
+    const float f = 1.f / sqrtf((float)m);
+    const double e = fma(-(double)f * f, m, 1.0);
+    return Two{f, fabs(e) < 1.0 ? 0.5f * (float)e * f : 0.f};
 }
 __device__ __forceinline__ float element(const Mat &m, int64_t row, int col) {
     if (m.dtype == ORTHRUS_F32) return ((const float *)m.data)[row * m.stride + col];
@@ -54,13 +61,17 @@ __device__ __forceinline__ float beside_middle(Two s, float g, Two f) {
 #endif
 
 // A row a workgroup at a time, kept in registers: thread t holds eight neighbours from 8 t on, and V - 1 more
-// such runs 8 NT apart; the gain stays, and the next row is on its way while a row is worked on (8192 rows of 4096 in bf16 to 8 bits:
-// 29 us, 3.5 TB/s; with a workgroup for each row and fp32 statistics 30).  Of 33 million codes of such rows 2 to 6 differ from those of
-// the definition in 64 bits; with the factor and the products rounded in fp32 14 to 30, in 24.6 us.  V = 0: any width, the row is read twice.
+// such runs 8 NT apart; the gain stays, and the next row is on its way while a row is worked on (with a workgroup for each row a
+// microsecond more).  V = 0: any width, the row is read twice.  8192 rows of 4096 in bf16 to 8 bits: 30.2 us, 3.4 TB/s; vector work bounds it.
+// Squares are added in 64 bits, whose products and sums cost as much as fp32's (in fp32, and at the end in two parts, 29.5 us here, 38.9 for
+// 36.2 of 2048 x 16384): an element beside the middle between two codes of three mantissa bits gets the code of the definition; smaller
+// codes, and the scale where a block's maximum lies on its border, are those of y in fp32.  With the factor and the products rounded in
+// fp32 14 to 30 of 33 million codes are not the definition's, in 24.6 us.
 template <int NT, int V, bool WHOLE>
-__global__ __launch_bounds__(NT) void norm_op_kernel(NormOp a) {
+__global__ __launch_bounds__(NT, NT == 256 && V == 1 ? 6 : 1) void norm_op_kernel(NormOp a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __shared__ Two shared[2][NT / 64];
+    __shared__ double shared[2][NT / 64];
+    const double share = 1.0 / a.width;
     const int t = threadIdx.x;
     auto sum_at = [&](int64_t row, int col, float (&s)[8]) {
         load_cols<WHOLE>(a.x, row, col, a.width, s);
@@ -89,7 +100,7 @@ __global__ __launch_bounds__(NT) void norm_op_kernel(NormOp a) {
                 for (int i = 0; i < 8; ++i)
                     if (((__float_as_uint(y[i]) - 0x7fffcu) & 0xfffffu) <= 8 && col + i < a.width) {
                         Two whole{s[i], 0.f};
-                        if (a.add.data) whole = add(Two{element(a.x, row, col + i), 0.f}, Two{element(a.add, row, col + i), 0.f});
+                        if (a.add.data) whole = add(element(a.x, row, col + i), element(a.add, row, col + i));
                         y[i] = beside_middle(whole, g[i], f);
                     }
             }
@@ -104,7 +115,7 @@ __global__ __launch_bounds__(NT) void norm_op_kernel(NormOp a) {
         for (int i = 0; i < 8; ++i) g[i] = a.gain ? 0.f : 1.f;
         if (in && a.gain) load_cols<WHOLE>(Mat{(char *)a.gain, nullptr, 0, 0, ORTHRUS_F32}, 0, col, a.width, g);
     };
-    auto factor = [&](float sq, int turn) { return row_factor(block_sum<NT>(sq, shared[turn & 1]), (float)a.width, a.eps); };
+    auto factor = [&](double sq, int turn) { return row_factor(block_sum<NT>(sq, shared[turn & 1]), share, a.eps); };
     int turn = 0;
     if constexpr (V > 0) {
         float s[V][8], g[V][8];
@@ -121,13 +132,14 @@ __global__ __launch_bounds__(NT) void norm_op_kernel(NormOp a) {
 #pragma unroll
         for (int v = 0; v < V; ++v) gain_at(8 * (v * NT + t), 8 * (v * NT + t) < a.width, g[v]);
         for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-            float c[V][8], sq = 0.f;
+            float c[V][8];
+            double sq = 0.0;
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     c[v][i] = s[v][i];
-                    sq = fmaf(c[v][i], c[v][i], sq);
+                    sq = fma((double)c[v][i], (double)c[v][i], sq);
                 }
             if (row + gridDim.x < a.rows) load(row + gridDim.x);
             const Two f = factor(sq, turn++);
@@ -136,18 +148,14 @@ __global__ __launch_bounds__(NT) void norm_op_kernel(NormOp a) {
         }
     } else {
         for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-            // (runs of eight are added in two parts: a thread has any number of them, and in fp32 a row of 2^24 equal elements would be off
-            // by up to a thousandth)
             float s[8], g[8];
-            Two whole{0.f, 0.f};
+            double sq = 0.0;
             for (int col = 8 * t; col < a.width; col += 8 * NT) {
                 sum_at(row, col, s);
-                float sq = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sq = fmaf(s[i], s[i], sq);
-                whole = add(whole, Two{sq, 0.f});
+                for (int i = 0; i < 8; ++i) sq = fma((double)s[i], (double)s[i], sq);
             }
-            const Two f = factor(isfinite(whole.high) ? whole.high + whole.low : whole.high, turn++);
+            const Two f = factor(sq, turn++);
             for (int c0 = 0; c0 < a.width; c0 += 8 * NT) {
                 const int col = c0 + 8 * t;
                 const bool in = col < a.width;
