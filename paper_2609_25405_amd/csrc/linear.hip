@@ -168,7 +168,7 @@ ProductPlan plan_product(const PackedShape &s, int rows, int groups, bool joint)
     }
     if (div_up(rows, groups) <= 16) {
         // One tile of 16 rows: the weights go straight to registers.  1 x 6144 x 4096 in 8 bits 7.3 us against 10.3, 8 x 4096 x 14336
-        // 12.9 against 15.5; with many columns the tiles are as fast
+        // 12.3 against 15.5; with many columns the tiles are as fast
         const double us = 2.0 + 1.25 * weight_us;
         if (us < best_us) {
             best.shape = -1;

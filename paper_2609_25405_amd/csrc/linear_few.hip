@@ -1,5 +1,5 @@
 // Products of few rows: tiles of at most 16 rows of x, bound by reading the weights once: 1 x 6144 x 4096 in 8 bits 6.6 us, 3.9 TB/s
-// with the launch (64 x 128 tiles in four parts of K: 10.3); 8 x 4096 x 14336 12.9, 4.6 TB/s (15.5).
+// with the launch (64 x 128 tiles in four parts of K: 10.3); 8 x 4096 x 14336 12.3, 4.8 TB/s (15.5).
 //
 // A workgroup owns NT tiles of 16 weight rows and one tile of x; its waves deal the steps
 // of K out among themselves, so that together they read one contiguous stream, keep DEPTH steps
@@ -100,7 +100,9 @@ template <int DT, int NT, int DEPTH, bool GATED> __global__ __launch_bounds__(64
 }
 
 template <int DT, int NT, bool GATED> hipError_t go(const Product &p, hipStream_t s) {
-    constexpr int DEPTH = NT == 4 ? 3 : 4;
+    // Two steps on their way in each of eight waves: three and four are as fast at most sizes (1 x 6144 x 4096 in 8 bits 7.3, 7.6, 7.4 us;
+    // 16 x 12300 x 2048 8.6, 8.5, 8.8) and slower where a wave has many steps (8 x 4096 x 14336 12.3, 12.8, 13.4)
+    constexpr int DEPTH = 2;
     hipLaunchKernelGGL((few_kernel<DT, NT, DEPTH, GATED>), dim3((unsigned)few_units(p.shape, p.rows, p.groups, NT)), dim3(64 * kWaves), 0, s, p);
     return hipGetLastError();
 }
