@@ -1,7 +1,7 @@
 // Products of more than a few rows, y = act(x W^T + bias) (* (x U^T + bias_u)) + residual: tiles of BM rows of x by BN weight
 // rows.  Large ones are bound by the chip's power and by what feeds the matrix cores: 4096 x 28672 x 4096 in 8 bits 400 us, 2.4
-// PFLOP/s, the matrix pipe 0.56 busy at 1.95 GHz (8192^3: 425 us, 2.59 PFLOP/s; without the copies into LDS 357, without the
-// epilogue 416); with few rows by the weights' bytes (64 x 28672 x 4096: 25 us, 4.7 TB/s).
+// PFLOP/s, the matrix pipe 0.57 busy at 1.93 GHz (8192^3: 440 us, 2.5 PFLOP/s; of an earlier 425 us 357 were left without the copies into LDS,
+// 416 without the epilogue); with few rows by the weights' bytes (64 x 28672 x 4096: 25 us, 4.7 TB/s).
 //  - A wave holds 128 x 128 sums of a 256 x 256 tile in its accumulation registers: per product the fewest bytes from LDS, whose reads
 //    and fills take three quarters of the products' time (of 128 x 256 all of it).
 //  - 32x32x64 fragments: a half step's operands are live at a time, not a step's, so that nothing spills (16x16x128: 599 us).

@@ -61,8 +61,9 @@ __device__ __forceinline__ float beside_middle(Two s, float g, Two f) {
 #endif
 
 // A row a workgroup at a time, kept in registers: thread t holds eight neighbours from 8 t on, and V - 1 more
-// such runs 8 NT apart; the gain stays, and the next row is on its way while a row is worked on (with a workgroup for each row a
-// microsecond more).  V = 0: any width, the row is read twice.  8192 rows of 4096 in bf16 to 8 bits: 30.2 us, 3.4 TB/s; vector work bounds it.
+// such runs 8 NT apart; the gain stays, and the next row is on its way while a row is worked on (30 -> 24.6 us at 8192 x 4096 with all in
+// fp32).  V = 0: any width, the row is read twice.  8192 rows of 4096 in bf16 to 8 bits: 30.2 us, 3.4 TB/s, to bf16 27.7, 4.8 TB/s; vector
+// work bounds the former.
 // Squares are added in 64 bits, whose products and sums cost as much as fp32's (in fp32, and at the end in two parts, 29.5 us here, 38.9 for
 // 36.2 of 2048 x 16384): an element beside the middle between two codes of three mantissa bits gets the code of the definition; smaller
 // codes, and the scale where a block's maximum lies on its border, are those of y in fp32.  With the factor and the products rounded in
@@ -170,7 +171,8 @@ __global__ __launch_bounds__(NT, NT == 256 && V == 1 ? 6 : 1) void norm_op_kerne
 #endif
 }
 
-// Blocks of rows: four lanes a block of 32.  Bound by memory, as the way back is (8192 x 4096 to bf16: 17.4 us, 5.9 TB/s).
+// Blocks of rows: four lanes a block of 32.  Bound by memory, as the way back is: 8192 x 4096 from bf16 23.2 us, 4.4 TB/s, from fp32 31.5, 5.4
+// TB/s; back to bf16 17.4 us, 5.9 TB/s.
 __global__ __launch_bounds__(256) void to_blocks_kernel(Mat x, Mat y, int rows, int width) {
 #if defined(__HIP_DEVICE_COMPILE__)
     const int per_row = (width + kBlock8 - 1) / kBlock8 * 4;
@@ -221,8 +223,8 @@ __global__ __launch_bounds__(256) void from_blocks_kernel(Mat x, Mat y, int rows
 hipError_t launch_norm_op(const NormOp &a, hipStream_t s) {
     auto go = [&](auto nt_c, auto v_c) {
         constexpr int NT = decltype(nt_c)::value, V = decltype(v_c)::value;
-        // What the CUs hold at once by their registers (94 of 512 a lane for two runs a thread): 8192 rows of 4096 with five workgroups
-        // a CU 29 us, with six 35, since the sixth then runs alone
+        // What the CUs hold at once by their registers (95 of 512 a lane for two runs a thread, 80 for one): 8192 rows of 4096 with five
+        // workgroups a CU 30 us, with six 35, since the sixth then runs alone
         constexpr int PER_CU = NT > 256 ? 1024 / NT : NT == 256 && V == 2 ? 5 : 1536 / NT;
         const int most = 256 * PER_CU, blocks = a.rows < most ? a.rows : most;
         if (a.width % 8 == 0) hipLaunchKernelGGL((norm_op_kernel<NT, V, true>), dim3(blocks), dim3(NT), 0, s, a);
@@ -232,6 +234,9 @@ hipError_t launch_norm_op(const NormOp &a, hipStream_t s) {
     constexpr std::integral_constant<int, 0> twice;
     constexpr std::integral_constant<int, 1> one;
     constexpr std::integral_constant<int, 2> two;
+    // The fewest waves that hold a row in two runs a thread, or in one where that is a wave or four.  65536 x 512 in bf16 to 8 bits: 29.7 us on
+    // 64 threads, 85.7 on 256; 16384 x 2048 30.2 on 256, 35.2 on 128 with two runs; 8192 x 4096 30.2, 40.0 on 512 with one; 4096 x 4104 and x 8192
+    // 22.4 and 32.4, on 1024 with one 27.5 and 41.5; 2048 x 16384 36.2, read twice 41.2
     if (a.width <= 512) return go(std::integral_constant<int, 64>{}, one);
     if (a.width <= 2048) return go(std::integral_constant<int, 256>{}, one);
     if (a.width <= 4096) return go(std::integral_constant<int, 256>{}, two);

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2609_25405_amd import linear as L
-from tests.linear_common import check, host, product_bound
+from tests.linear_common import check, host, mx_values, product_bound
 
 pytestmark = pytest.mark.gpu
 
@@ -194,3 +194,21 @@ def test_wide_rows_past_the_range():
         y = torch.full_like(x, 5.0)
         L.norm(x, y)
         assert (y[0] == 0).all() and y[1].isnan().all() and ((y[2] - 1).abs() < 1e-4).all()
+
+
+@pytest.mark.parametrize("rows", [9, 200])
+def test_blocks_read_back_give_exact_products(rows):
+    """What the matrix cores cut of 8-bit products is all there in bfloat16 products of the same values."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(rows)
+    n, k = 100, 1000
+    x8, w8 = L.Mx8.empty(rows, k), L.Mx8.empty(n, k)
+    for m in (x8, w8):
+        L.convert(torch.randn(m.shape, generator=gen, device="cuda") * torch.exp(2 * torch.randn((1, k), generator=gen, device="cuda")), m)
+    x, w = (torch.empty(m.shape, dtype=torch.bfloat16, device="cuda") for m in (x8, w8))
+    L.convert(x8, x)
+    L.convert(w8, w)
+    y = torch.empty((rows, n), device="cuda")
+    weights = L.LinearWeights(w)
+    L.linear(weights, L.aligned(x), y, workspace=L.linear_workspace(weights, rows))
+    check(y, *product_bound(mx_values(x8)[0], mx_values(w8)[0], None, None, None, None, "bf16"), rows)
