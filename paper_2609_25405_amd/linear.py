@@ -68,14 +68,25 @@ class Mx8:
 Rows = Union[torch.Tensor, Mx8]
 
 
-def aligned(t: torch.Tensor) -> torch.Tensor:
-    """``t`` [rows][k], or a copy of it, whose rows begin at multiples of 16 bytes, as the products read them."""
+def _aligned(t: torch.Tensor, to: int) -> torch.Tensor:
     es = t.element_size()
-    if t.stride(1) in (1,) and t.data_ptr() % 16 == 0 and (t.shape[0] < 2 or t.stride(0) * es % 16 == 0):
+    if t.stride(1) == 1 and t.data_ptr() % to == 0 and (t.shape[0] < 2 or t.stride(0) * es % to == 0):
         return t
-    room = torch.empty((t.shape[0], _up(t.shape[1] * es, 16) // es), dtype=t.dtype, device=t.device)[:, :t.shape[1]]
-    room.copy_(t)
+    room = torch.empty((t.shape[0], _up(t.shape[1] * es, to) // es), dtype=t.dtype, device=t.device)[:, :t.shape[1]]
+    if es == 1:
+        room.view(torch.uint8).copy_(t.view(torch.uint8))
+    else:
+        room.copy_(t)
     return room
+
+
+def aligned(t: Rows) -> Rows:
+    """``t`` [rows][k] if its rows begin where the products read them, at multiples of 16 bytes (scales of 8-bit blocks: of 4), else
+    with a copy, on the current stream, of what does not."""
+    if t.__class__ is not Mx8:
+        return _aligned(t, 16)
+    codes, scales = _aligned(t.codes, 16), _aligned(t.scales, 4)
+    return t if codes is t.codes and scales is t.scales else Mx8(codes, scales)
 
 
 def _row_stride(t: torch.Tensor, what: str) -> int:

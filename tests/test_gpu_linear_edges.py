@@ -212,3 +212,20 @@ def test_blocks_read_back_give_exact_products(rows):
     weights = L.LinearWeights(w)
     L.linear(weights, L.aligned(x), y, workspace=L.linear_workspace(weights, rows))
     check(y, *product_bound(mx_values(x8)[0], mx_values(w8)[0], None, None, None, None, "bf16"), rows)
+
+
+@pytest.mark.parametrize("rows,k", [(5, 70), (90, 333)])
+def test_rows_that_begin_anywhere_once_aligned(rows, k):
+    """8-bit rows side by side without padding, refused as they lie, give the product of the same rows laid out."""
+    m, w8 = L.Mx8.empty(rows, k), L.Mx8.empty(40, k)
+    for t in (m, w8):
+        L.convert(torch.randn(t.shape, device="cuda"), t)
+    packed = L.Mx8(*[t.view(torch.uint8).contiguous().view(t.dtype) for t in (m.codes, m.scales)])
+    w = L.LinearWeights(w8)
+    y, z = (torch.empty((rows, 40), device="cuda") for _ in range(2))
+    ws = L.linear_workspace(w, rows)
+    L.linear(w, m, y, workspace=ws)
+    with pytest.raises(L.A.OrthrusError):
+        L.linear(w, packed, z, workspace=ws)
+    L.linear(w, L.aligned(packed), z, workspace=ws)
+    assert torch.equal(y, z)

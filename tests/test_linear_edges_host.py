@@ -254,3 +254,20 @@ def test_workspaces_hold_every_smaller_call_and_only_cut_sums_need_one(dtype, n,
         if shape.steps < 8 or n > 150000:            # parts of fewer than four steps, or more tiles than two rounds: never cut
             assert room(8192) == room(1) == 0
     assert cut > 0 or n > 20000
+
+
+# ------------------------------------------------------------------------------ where rows begin
+@pytest.mark.parametrize("rows,width,pad,off", [(3, 64, 0, 0), (3, 128, 0, 0), (1, 33, 3, 0), (4, 130, 6, 0), (4, 128, 16, 16), (4, 100, 12, 4), (5, 1, 0, 0)])
+def test_aligned_rows_are_the_same_or_a_copy(rows, width, pad, off):
+    nb = -(-width // 32)
+    codes = torch.arange(rows * (width + pad + off), dtype=torch.uint8).view(rows, -1)[:, off:off + width].view(torch.float8_e4m3fn)
+    scales = torch.arange(rows * (nb + pad), dtype=torch.uint8).view(rows, -1)[:, :nb].view(torch.float8_e8m0fnu)
+    m = L.Mx8(codes, scales)
+    a = L.aligned(m)
+    assert torch.equal(a.codes.view(torch.uint8), codes.view(torch.uint8)) and torch.equal(a.scales.view(torch.uint8), scales.view(torch.uint8))
+    for t, kept, to in ((a.codes, codes, 16), (a.scales, scales, 4)):
+        fits = lambda t: t.data_ptr() % to == 0 and (rows == 1 or t.stride(0) % to == 0)
+        assert fits(t) and (t.data_ptr() == kept.data_ptr()) == fits(kept)
+    assert L.aligned(a) is a
+    b = torch.zeros((rows, width + 1), dtype=torch.bfloat16)[:, 1:]
+    assert L.aligned(b).data_ptr() % 16 == 0 and L.aligned(L.aligned(b)).shape == b.shape
