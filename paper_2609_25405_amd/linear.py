@@ -39,7 +39,9 @@ class Mx8:
         self._tensors, self._shape = (codes, scales), codes.shape
         self._device = codes.get_device()
         _need(scales.get_device() == self._device, "codes and scales on one device")
-        self._ref = _pack(codes.data_ptr(), scales.data_ptr(), _row_stride(codes, "codes"), _row_stride(scales, "scales"), L.ORTHRUS_MX8)
+        at, scales_at, stride, scale_stride = codes.data_ptr(), scales.data_ptr(), _row_stride(codes, "codes"), _row_stride(scales, "scales")
+        self._ref = _pack(at, scales_at, stride, scale_stride, L.ORTHRUS_MX8)
+        self._aligned = (at | stride) % 16 == 0 and (scales_at | scale_stride) % 4 == 0
 
     @classmethod
     def empty(cls, rows: int, width: int, device="cuda") -> "Mx8":
@@ -85,8 +87,7 @@ def aligned(t: Rows) -> Rows:
     with a copy, on the current stream, of what does not."""
     if t.__class__ is not Mx8:
         return _aligned(t, 16)
-    codes, scales = _aligned(t.codes, 16), _aligned(t.scales, 4)
-    return t if codes is t.codes and scales is t.scales else Mx8(codes, scales)
+    return t if t._aligned else Mx8(_aligned(t.codes, 16), _aligned(t.scales, 4))
 
 
 def _row_stride(t: torch.Tensor, what: str) -> int:
