@@ -187,9 +187,8 @@ def prepare(case, seed):
         from paper_2609_25405_amd import linear as L
 
         mx8 = case["dtype"] == "mx8"
-        # codes and scales as they lie, if the products read them so; else the call lays them out
-        if mx8 and st["x"][0].stride(0) % 16 == 0 and st["x"][1].stride(0) % 4 == 0:
-            st["own_x"] = L.Mx8(st["x"][0], st["x"][1].view(torch.float8_e8m0fnu))
+        # as it lies: what the products do not read so is laid out by the call
+        st["own_x"] = L.Mx8(st["x"][0], st["x"][1].view(torch.float8_e8m0fnu)) if mx8 else st["x"]
         mats = [L.Mx8.of(*w) if mx8 else w for w in st["w"]]
         st["weights"] = L.LinearWeights(mats[0], up=mats[1] if W == 2 else None, groups=G)
         st["y"] = torch.empty((R, N), dtype=_torch_dtype(case["y"]), device=dev)
@@ -211,7 +210,7 @@ def run(st):
                 y = st["read"]
             return (y,) if st["total"] is None else (y, st["total"])
         after = dict(bias=st["bias"], act=case["act"] or None, residual=st["residual"], workspace=st["ws"])
-        x = st.get("own_x") or (L.Mx8.of(*st["x"]) if case["dtype"] == "mx8" else L.aligned(st["x"]))
+        x = L.aligned(st["own_x"])
         if case["op"] == "linear":
             L.linear(st["weights"], x, st["y"], **after)
         else:
