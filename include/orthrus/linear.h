@@ -52,10 +52,10 @@ int orthrus_convert(const orthrus_matrix *x, const orthrus_matrix *y, int32_t ro
 /* RMS norm of each row, after the addition of a residual: s = x + add (fp32; add NULL: s = x),
  * total = s rounded to its type (total NULL: not written), y = s * gain / sqrt(mean(s^2) + eps) in y's type
  * (gain fp32 device [width]; NULL: ones).  x, add, total: F32 or BF16; y: F32, BF16 or MX8.  total
- * or y may be x or add itself (data, stride and dtype, not MX8); else what is written shares no byte with anything (EINVAL).  The mean is taken in 64
- * bits of s as fp32 holds it: y is off by at most 2^-22 of itself, and half a step of its type (squares whose sum passes fp32's range make a row
- * zero; 8-bit codes with three bits of mantissa are rounded once, from s before
- * its rounding).  Any strides >= width and any alignment to an element.
+ * or y may be x or add itself (data, stride and dtype, not MX8); else what is written shares no byte with anything (EINVAL).
+ * The mean is taken in 64 bits of s as fp32 holds it: y is off by at most 2^-22 of itself, and half a step of its type (squares whose sum
+ * passes fp32's range make a row zero; 8-bit codes with three bits of mantissa are rounded once, from s before its rounding).  Any
+ * strides >= width and any alignment to an element.
  * EINVAL: a null pointer, width < 1, eps negative or not a number; ECAPACITY: width > 2^30. */
 int orthrus_norm(const orthrus_matrix *x, const orthrus_matrix *add, const orthrus_matrix *total, const float *gain, float eps,
                  const orthrus_matrix *y, int32_t rows, int32_t width, void *stream);
@@ -91,13 +91,16 @@ size_t orthrus_linear_bytes(const orthrus_linear_weights *w, int32_t rows);
 
 /* y[r] = act(x[r] W^T + bias) + residual[r], or for gated weights act(x W^T + bias) * (x U^T + bias_u) +
  * residual; w->groups is 1.  x: rows of k elements of the weights' type; 16-byte aligned, row stride a multiple of 16
- * bytes; for MX8 scales 4-byte aligned, scale_stride a multiple of 4 (the 16 bytes, of scales the 4, that hold a row's last
- * elements are read whole, what lies between rows may be read, and nothing outside of these is).  y: rows of n elements, F32, BF16 or MX8, any stride and alignment to an element.  epilogue NULL:
- * none.  Sums in fp32, in an order that depends on the sizes alone; bf16 products are exact.  The matrix cores add 8-bit
- * products eight neighbours at a time, without the bits below 2^-13 of the power of two of the largest of the eight: 1.5e-5 of a sum of
- * normal data.  Where that counts, blocks that orthrus_convert reads back to BF16 go through weights packed in BF16, exactly, at half the rate.
+ * bytes; for MX8 scales 4-byte aligned, scale_stride a multiple of 4.  The 16 bytes, of scales the 4, that hold a row's last
+ * elements are read whole, what lies between rows may be read, and nothing outside of these is.  y: rows of n elements, F32, BF16 or
+ * MX8, any stride and alignment to an element.  epilogue NULL: none.
+ *
+ * Sums in fp32, in an order that depends on the sizes alone; bf16 products are exact.  The matrix cores add 8-bit products eight
+ * neighbours at a time, without the bits below 2^-13 of the power of two of the largest of the eight: 1.5e-5 of a sum of normal data.  Where
+ * that counts, blocks that orthrus_convert reads back to BF16 go through weights packed in BF16, exactly, at half the rate.
+ *
  * workspace: 16-byte aligned, one call in flight; calls may be captured into graphs.  EINVAL: null pointers, sizes, strides or
- * alignments against the above; EUNSUPPORTED: types without a kernel; ECAPACITY: workspace too small; k > 2^22,
+ * alignments against the above, memory that is shared; EUNSUPPORTED: types without a kernel; ECAPACITY: workspace too small; k > 2^22,
  * n > 2^26 or rows >= 2^30; 2^31 bytes or more in 256 rows of x or of its scales; more tiles than a launch holds (2^24 of 64 rows by 128
  * weight rows or more; 2^23 of 16 by 16 or more where a group's share is at most 16 rows).  rows = 0 is a no-op. */
 int orthrus_linear(const orthrus_linear_weights *w, const orthrus_matrix *x, int32_t rows, const orthrus_epilogue *epilogue,
